@@ -421,6 +421,107 @@ fd_status fd_gemm_e4m3_device(const uint8_t* a, int64_t lda, const float* a_scal
                               int32_t m, int32_t n, int32_t k, int32_t epilogue, void* out,
                               int64_t ld_out, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Rotary positions, and a key / value cache with a token budget: the decoder's
+ * 3D-RoPE, ring append and ring attention (Sec. 3.2, 3.3) as operators on caller
+ * memory, for caches that keep the tokens attention looks at rather than the last
+ * W_frm frames. Device pointers unless said otherwise, on the current HIP device;
+ * asynchronous on `stream` (NULL = default); nothing is allocated, so every call
+ * may be captured into a HIP graph. Arguments are checked as far as the host sees
+ * them (FD_ERR_INVALID_ARGUMENT; FD_ERR_UNSUPPORTED for sizes that are not built),
+ * before any device work; a launch failure gives DEVICE.
+ * ------------------------------------------------------------------------ */
+
+/* Which elements of a head vector form pair i of rot_dim / 2. */
+enum { FD_ROPE_INTERLEAVED = 0, /* (2 i, 2 i + 1), the decoder's 3D-RoPE        */
+       FD_ROPE_HALF = 1 };      /* (i, i + rot_dim / 2)                         */
+
+/* How frequencies are scaled for contexts longer than the trained one. */
+enum { FD_ROPE_SCALE_NONE = 0,
+       FD_ROPE_SCALE_LINEAR = 1, /* every frequency / factor                     */
+       FD_ROPE_SCALE_BASE = 2,   /* theta factor^(h / (h - 1)), h = rot_dim / 2: the
+                                    slowest pair / factor, the fastest unchanged */
+       FD_ROPE_SCALE_BANDS = 3 };/* pairs of at least fast_turns turns over the
+                                    trained length unchanged, of at most slow_turns
+                                    / factor, in between a linear mix of both    */
+
+/* A rotation: pair i turns by the angle coordinate[axis[i]] freq[i],
+ *   (x0, x1) -> magnitude (x0 cos - x1 sin, x0 sin + x1 cos);
+ * elements from rot_dim on are copied. The angle is reduced in fp64. inverse turns
+ * back (the gradient of a rotation is its inverse at the same magnitude). */
+typedef struct fd_rope {
+  uint32_t struct_size;   /* must be sizeof(fd_rope) (ABI guard)                 */
+  int32_t rot_dim;        /* rotated elements, even, 0 .. head_dim               */
+  int32_t layout;         /* FD_ROPE_INTERLEAVED / FD_ROPE_HALF                  */
+  int32_t n_axes;         /* coordinates per token, 1 .. 4                       */
+  const double* freq;     /* [rot_dim / 2], radians per unit of the coordinate   */
+  const int32_t* axis;    /* [rot_dim / 2] coordinate of each pair (limited to
+                             0 .. n_axes - 1), or NULL: all 0                    */
+  float magnitude;        /* multiplies cos and sin                              */
+  int32_t inverse;        /* 1: turn back                                        */
+} fd_rope;
+
+/* Frequencies of rot_dim / 2 pairs, theta^(-2 i / rot_dim) with the scaling above,
+ * into freq (host), and the magnitude that goes with it (host): 1, or
+ * 1 + 0.1 ln(factor) for FD_ROPE_SCALE_BANDS. factor >= 1 (unused for NONE);
+ * trained_length, fast_turns > slow_turns >= 0 for BANDS only. Several axes: one
+ * call per axis, the results joined. rot_dim even, 2 .. 512. Host only. */
+fd_status fd_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double trained_length,
+                              double fast_turns, double slow_turns, double* freq, float* magnitude);
+
+/* Rotate the head vectors x[token][head][0 .. head_dim) (dtype; strides in
+ * elements, any alignment) at coords[token][n_axes] into out, computed in fp32 and
+ * rounded once. out may be x with the same strides and must not overlap it
+ * otherwise. tokens in [0, 2^31), heads 1 .. 65536, head_dim 1 .. 512. */
+fd_status fd_rope_device(const fd_rope* rope, const void* x, int32_t dtype, int64_t tokens, int32_t heads,
+                         int32_t head_dim, int64_t x_token_stride, int64_t x_head_stride, const int32_t* coords,
+                         void* out, int64_t out_token_stride, int64_t out_head_stride, void* stream);
+
+#define FD_TOKEN_MAX_CAPACITY (1 << 24)
+
+/* A token cache: for each request and KV group `capacity` slots of one key, one
+ * value, a position and a weight. The order of slots means nothing: what a query sees goes
+ * by positions alone. The caller owns the memory; a new cache has every pos < 0 (empty;
+ * K, V and weight of empty slots may hold anything). 16-byte aligned k and v rows. */
+typedef struct fd_token_cache {
+  uint32_t struct_size;   /* must be sizeof(fd_token_cache) (ABI guard)          */
+  int32_t dtype;          /* fd_dtype of k and v                                 */
+  int32_t batch, groups;  /* batch x groups <= 65535                             */
+  int32_t capacity;       /* slots, 1 .. FD_TOKEN_MAX_CAPACITY                   */
+  int32_t head_dim;       /* 32, 64 or 128, else UNSUPPORTED                     */
+  void* k;                /* [batch][groups][capacity][head_dim] by strides      */
+  void* v;
+  int64_t k_stride[3];    /* batch, group, slot, in elements: whole 16 bytes and */
+  int64_t v_stride[3];    /*   at least head_dim                                 */
+  int32_t* pos;           /* [batch][groups][capacity], < 0: empty               */
+  float* weight;          /* [batch][groups][capacity], accumulated attention    */
+} fd_token_cache;
+
+/* Choose slots for n new tokens per request at positions pos[batch][n] (< 0: padding,
+ * gets slot -1). In every (request, group), slots are ordered by class, then weight,
+ * then index; classes: 0 empty, 1 any other, 2 recent (slot_pos > newest -
+ * keep_recent, newest = the request's largest new position), 3 first (slot_pos <
+ * keep_first). The first m of them, in rising order, go to the request's m valid
+ * tokens in order: empty slots are filled first, then the least attended tokens are
+ * replaced, recent and first ones only when no other is left. NaN weights order as
+ * -infinity, -0 as 0. slot_pos, weight [batch][groups][capacity] are read only; slots
+ * [batch][groups][n]. n <= capacity and n <= 65536, keep_first, keep_recent >= 0. */
+fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, int32_t batch, int32_t groups,
+                                int32_t capacity, const int32_t* pos, int32_t n, int32_t keep_first,
+                                int32_t keep_recent, int32_t* slots, void* stream);
+
+/* Write n new tokens per request into their slots: k (rotated by `rope` at
+ * coords[batch][n][n_axes], computed in fp32 and rounded once; NULL rope: as it is) and v,
+ * both [batch][n][groups][head_dim] of the cache's dtype by strides (host arrays:
+ * batch, token, group; whole 16 bytes, rows 16-byte aligned), pos, and weight 0.
+ * coords NULL: pos is the one coordinate. Tokens with pos < 0 or a slot outside
+ * [0, capacity) are left out. The slots of one (request, group) must differ, as
+ * fd_token_slots_device's do: where two tokens name one slot, it is left with
+ * parts of both. */
+fd_status fd_token_append_device(const fd_token_cache* cache, const fd_rope* rope, const void* k,
+                                 const int64_t k_stride[3], const void* v, const int64_t v_stride[3], int32_t n,
+                                 const int32_t* pos, const int32_t* coords, const int32_t* slots, void* stream);
+
 const char* fd_status_string(fd_status status);
 
 /* Message of the last failed call on this thread ("" if none). */

@@ -13,13 +13,14 @@
 #include <string>
 #include <vector>
 
+#include "fd_error.h"
 #include "fd_kernels.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+}
 
-fd_status fail(fd_status st, const char* fmt, ...) {
+fd_status fd::fail(fd_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -28,6 +29,10 @@ fd_status fail(fd_status st, const char* fmt, ...) {
   g_last_error = buf;
   return st;
 }
+
+namespace {
+
+using fd::fail;
 
 #define FD_HIP(expr)                                                                   \
   do {                                                                                 \

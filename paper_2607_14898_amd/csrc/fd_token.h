@@ -1,0 +1,66 @@
+// Internal interface between the host checks of the token cache and of rotary
+// positions (fd_token.cpp) and their gfx950 kernels. Every launcher enqueues on
+// `stream` and returns the hipError_t of the launch; shapes are checked before.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace fd {
+
+// Rotation of the first 2 half elements of a head vector.
+struct RopeArgs {
+  const double* freq = nullptr;   // [half] angular frequency of each pair
+  const int* axis = nullptr;      // [half] coordinate that turns the pair, or null (all 0)
+  const int* coords = nullptr;    // [tokens][axes]
+  int axes = 1, half = 0;
+  int interleaved = 1;            // pairs (2 i, 2 i + 1); else (i, i + half)
+  float mag = 1.f;                // cos and sin are multiplied by this
+  float sign = 1.f;               // -1: the inverse rotation
+};
+
+struct RopeRows {
+  const void* x = nullptr;
+  void* out = nullptr;
+  int64_t tokens = 0;
+  int heads = 1, dim = 64;
+  int64_t x_token = 0, x_head = 0, o_token = 0, o_head = 0;  // strides in elements
+};
+
+// kind: 0 f16, 1 bf16, 2 fp32
+hipError_t rope_rows(const RopeArgs& r, const RopeRows& x, int kind, hipStream_t stream);
+
+// A token cache's memory (strides in elements: batch, group, slot).
+struct TokenCacheArgs {
+  void* k = nullptr;
+  void* v = nullptr;
+  int* pos = nullptr;        // [B][G][C], < 0: empty
+  float* weight = nullptr;   // [B][G][C]
+  int64_t ks[3] = {}, vs[3] = {};
+  int B = 1, G = 1, C = 1, D = 64;
+};
+
+struct TokenAppend {
+  const void* k = nullptr;   // [B][n][G][D] by strides (batch, token, group)
+  const void* v = nullptr;
+  int64_t ks[3] = {}, vs[3] = {};
+  int n = 0;
+  const int* pos = nullptr;    // [B][n]
+  const int* slots = nullptr;  // [B][G][n]
+};
+// Rotated keys (r.half 0: as they are) and values into their slots.
+hipError_t token_append(const TokenCacheArgs& c, const RopeArgs& r, const TokenAppend& a, int kind,
+                        hipStream_t stream);
+
+struct TokenSlots {
+  const int* slot_pos = nullptr;   // [B][G][C]
+  const float* weight = nullptr;   // [B][G][C]
+  const int* pos = nullptr;        // [B][n]
+  int* slots = nullptr;            // [B][G][n]
+  int B = 1, G = 1, C = 1, n = 1;
+  int keep_first = 0, keep_recent = 0;
+};
+constexpr int kMaxSlotTokens = 65536;  // new tokens of one choice
+hipError_t token_slots(const TokenSlots& a, hipStream_t stream);
+
+}  // namespace fd

@@ -45,6 +45,19 @@ class fd_tensor_desc(ctypes.Structure):
                 ("shape", ctypes.c_int64 * 2), ("offset", ctypes.c_uint64)]
 
 
+class fd_rope(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("magnitude", ctypes.c_float), ("inverse", ctypes.c_int32)]
+
+
+class fd_token_cache(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("pos", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
+
+
 class FlashDecoderError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"[{status}] {msg}")
@@ -101,6 +114,11 @@ def load_library() -> ctypes.CDLL:
         "fd_set_fp8_act_amax": (I32, [P, P, SZ]),
         "fd_calibrate_chunk": (I32, [P, P, I32, I32, P, P, P, SZ, P]),
         "fd_gemm_e4m3_device": (I32, [P, I64, P, P, P, P, I32, I32, I32, I32, P, I64, P]),
+        "fd_rope_frequencies": (I32, [I32, ctypes.c_double, I32] + [ctypes.c_double] * 4 +
+                                [P, ctypes.POINTER(ctypes.c_float)]),
+        "fd_rope_device": (I32, [P, P, I32, I64, I32, I32, I64, I64, P, P, I64, I64, P]),
+        "fd_token_slots_device": (I32, [P, P, I32, I32, I32, P, I32, I32, I32, P, P]),
+        "fd_token_append_device": (I32, [P, P, P, P, P, P, I32, P, P, P, P]),
         "fd_status_string": (ctypes.c_char_p, [I32]),
         "fd_last_error": (ctypes.c_char_p, []),
     }
@@ -473,3 +491,196 @@ def decode_chunks(caches, latents, outs=None, out_format: int = FD_PIXELS_F32, s
                             device=z.device) for c, z in zip(caches, latents)]
     fd_decode_chunks(dec.handle, latents, F, [c.handle for c in caches], outs, out_format, stream)
     return outs
+
+
+# ------------------------------------------------------------------ rotary positions and the token cache
+
+FD_ROPE_INTERLEAVED, FD_ROPE_HALF = 0, 1
+_ROPE_LAYOUTS = {"interleaved": FD_ROPE_INTERLEAVED, "half": FD_ROPE_HALF}
+_ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> None:
+    """ValueError unless t is a CUDA tensor of this dtype, shape and device, contiguous
+    (strided: along its last dimension only)."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{name} must be on {device or 'a GPU'}, got {t.device}")
+    if not (t.is_contiguous() or (strided and (t.shape[-1] <= 1 or t.stride(-1) == 1))):
+        raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
+
+
+def _dtype_code(t, name: str) -> int:
+    import torch
+    code = {torch.float32: FD_DTYPE_F32, torch.bfloat16: FD_DTYPE_BF16, torch.float16: FD_DTYPE_F16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _call_on(device, stream, fn, *args) -> None:
+    """fn(*args, stream) with `device` current; stream defaults to its current one."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream of {stream.device} for tensors on {device}")
+    if torch.cuda.current_device() == device.index:
+        st = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, stream.cuda_stream)
+    if st != FD_OK:
+        _check(st)
+
+
+def _new(shape, dtype, device, stream):
+    """An uninitialised tensor that work on `stream` may use until it is done."""
+    import torch
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def fd_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                        trained_length: float = 0.0, fast_turns: float = 32.0, slow_turns: float = 1.0):
+    """(frequencies float64 numpy [rot_dim / 2], magnitude) of a rotary embedding;
+    scaling "none", "linear", "base" or "bands"."""
+    freq = np.empty(max(rot_dim, 0) // 2, np.float64)
+    mag = ctypes.c_float()
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(_ROPE_SCALINGS)}")
+    _check(load_library().fd_rope_frequencies(rot_dim, theta, _ROPE_SCALINGS[scaling], factor, trained_length,
+                                              fast_turns, slow_turns, freq.ctypes.data, ctypes.byref(mag)))
+    return freq, mag.value
+
+
+class Rope:
+    """Rotary positions (fd_rope): frequencies of the pairs (float64, numpy or a GPU
+    tensor), and the coordinate that turns each pair (axis, int32; None: one axis)."""
+
+    def __init__(self, freq, axis=None, n_axes: int = 1, layout: str = "interleaved", magnitude: float = 1.0,
+                 inverse: bool = False, device="cuda"):
+        import torch
+        if layout not in _ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_ROPE_LAYOUTS)}")
+        if not isinstance(freq, torch.Tensor):
+            freq = torch.from_numpy(np.ascontiguousarray(freq, np.float64)).to(device)
+        _need(freq, "freq", torch.float64, freq.shape if freq.dim() == 1 else (freq.numel(),))
+        if axis is not None:
+            if not isinstance(axis, torch.Tensor):
+                axis = torch.from_numpy(np.ascontiguousarray(axis, np.int32)).to(freq.device)
+            _need(axis, "axis", torch.int32, freq.shape, freq.device)
+        self.freq, self.axis, self.n_axes = freq, axis, n_axes
+        self._s = fd_rope(ctypes.sizeof(fd_rope), 2 * freq.numel(), _ROPE_LAYOUTS[layout], n_axes, freq.data_ptr(),
+                          None if axis is None else axis.data_ptr(), magnitude, int(inverse))
+        self._p = ctypes.addressof(self._s)
+        self._args = (layout, magnitude, inverse)
+
+    def inverted(self) -> "Rope":
+        """The opposite rotation (its result is also the gradient of this one)."""
+        layout, magnitude, inverse = self._args
+        return Rope(self.freq, self.axis, self.n_axes, layout, magnitude, not inverse)
+
+    def __call__(self, x, coords, out=None, stream=None):
+        """Rotate x [tokens, heads, head_dim] (fp32, bf16 or fp16; strided) at coords
+        [tokens] or [tokens, n_axes] (int32); out may be x."""
+        import torch
+        tokens, heads, dim = x.shape
+        dt, dev = _dtype_code(x, "x"), self.freq.device
+        _need(x, "x", x.dtype, x.shape, dev, strided=True)
+        _need(coords, "coords", torch.int32, (tokens, self.n_axes) if coords.dim() == 2 or self.n_axes > 1 else (tokens,),
+              dev)
+        if out is None:
+            out = _new(x.shape, x.dtype, dev, stream)
+        else:
+            _need(out, "out", x.dtype, x.shape, dev, strided=True)
+        _call_on(dev, stream, load_library().fd_rope_device, self._p, x.data_ptr(), dt, tokens, heads, dim,
+                 x.stride(0), x.stride(1), coords.data_ptr(), out.data_ptr(), out.stride(0), out.stride(1))
+        return out
+
+
+def fd_token_slots_device(slot_pos, weight, pos, slots, keep_first: int = 0, keep_recent: int = 0,
+                          stream=None) -> None:
+    """Slots (int32 [batch, groups, n]) for n new tokens at pos (int32 [batch, n], < 0:
+    padding) of a cache with positions slot_pos and weights [batch, groups, capacity]."""
+    import torch
+    B, G, C = slot_pos.shape
+    n, dev = pos.shape[-1], slot_pos.device
+    _need(slot_pos, "slot_pos", torch.int32, slot_pos.shape)
+    _need(weight, "weight", torch.float32, slot_pos.shape, dev)
+    _need(pos, "pos", torch.int32, (B, n), dev)
+    _need(slots, "slots", torch.int32, (B, G, n), dev)
+    _call_on(dev, stream, load_library().fd_token_slots_device, slot_pos.data_ptr(), weight.data_ptr(), B, G, C,
+             pos.data_ptr(), n, keep_first, keep_recent, slots.data_ptr())
+
+
+class TokenCache:
+    """A key / value cache with a token budget over caller tensors: k, v [batch, groups,
+    capacity, head_dim] (strided), pos int32 and weight fp32 [batch, groups, capacity].
+
+    A step of a stream: ``insert`` the new tokens' keys and values (the least attended
+    tokens make room), then ``attend`` with their queries, which adds to the weights."""
+
+    def __init__(self, k, v, pos, weight):
+        import torch
+        B, G, C, D = k.shape
+        dt, dev = _dtype_code(k, "k"), k.device
+        _need(k, "k", k.dtype, k.shape, None, strided=True)
+        _need(v, "v", k.dtype, k.shape, dev, strided=True)
+        _need(pos, "pos", torch.int32, (B, G, C), dev)
+        _need(weight, "weight", torch.float32, (B, G, C), dev)
+        self.k, self.v, self.pos, self.weight = k, v, pos, weight
+        self.batch, self.groups, self.capacity, self.head_dim = B, G, C, D
+        I3 = ctypes.c_int64 * 3
+        self._s = fd_token_cache(ctypes.sizeof(fd_token_cache), dt, B, G, C, D, k.data_ptr(), v.data_ptr(),
+                                 I3(*k.stride()[:3]), I3(*v.stride()[:3]), pos.data_ptr(), weight.data_ptr())
+        self._p = ctypes.addressof(self._s)
+
+    @classmethod
+    def empty(cls, batch: int, groups: int, capacity: int, head_dim: int, dtype, device="cuda") -> "TokenCache":
+        """A cache with memory of its own and every slot empty."""
+        import torch
+        shape = (batch, groups, capacity)
+        k, v = (torch.zeros(*shape, head_dim, dtype=dtype, device=device) for _ in range(2))
+        return cls(k, v, torch.full(shape, -1, dtype=torch.int32, device=device),
+                   torch.zeros(shape, dtype=torch.float32, device=device))
+
+    def reset(self) -> None:
+        """Forget every token (on the current stream)."""
+        self.pos.fill_(-1)
+
+    def choose(self, pos, keep_first: int = 0, keep_recent: int = 0, stream=None):
+        """Slots [batch, groups, n] for new tokens at pos [batch, n] (fd_token_slots_device)."""
+        import torch
+        slots = _new((self.batch, self.groups, pos.shape[-1]), torch.int32, self.pos.device, stream)
+        fd_token_slots_device(self.pos, self.weight, pos, slots, keep_first, keep_recent, stream)
+        return slots
+
+    def append(self, k, v, pos, slots, rope: Optional[Rope] = None, coords=None, stream=None) -> None:
+        """Write k (rotated by rope at coords [batch, n, n_axes], default pos) and v
+        [batch, n, groups, head_dim] into their slots (fd_token_append_device)."""
+        import torch
+        dev, n = self.pos.device, pos.shape[-1]
+        shape = (self.batch, n, self.groups, self.head_dim)
+        _need(k, "k", self.k.dtype, shape, dev, strided=True)
+        _need(v, "v", self.k.dtype, shape, dev, strided=True)
+        _need(pos, "pos", torch.int32, (self.batch, n), dev)
+        _need(slots, "slots", torch.int32, (self.batch, self.groups, n), dev)
+        if coords is not None:
+            _need(coords, "coords", torch.int32, (self.batch, n, rope.n_axes if rope else 1), dev)
+        if rope is not None and rope.freq.device != dev:
+            raise ValueError(f"rope on {rope.freq.device} for a cache on {dev}")
+        I3 = ctypes.c_int64 * 3
+        _call_on(dev, stream, load_library().fd_token_append_device, self._p, None if rope is None else rope._p,
+                 k.data_ptr(), I3(*k.stride()[:3]), v.data_ptr(), I3(*v.stride()[:3]), n, pos.data_ptr(),
+                 None if coords is None else coords.data_ptr(), slots.data_ptr())
+
+    def insert(self, k, v, pos, rope: Optional[Rope] = None, coords=None, keep_first: int = 0,
+               keep_recent: int = 0, stream=None):
+        """choose, then append; returns the slots."""
+        slots = self.choose(pos, keep_first, keep_recent, stream)
+        self.append(k, v, pos, slots, rope, coords, stream)
+        return slots
