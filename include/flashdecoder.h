@@ -522,6 +522,37 @@ fd_status fd_token_append_device(const fd_token_cache* cache, const fd_rope* rop
                                  const int64_t k_stride[3], const void* v, const int64_t v_stride[3], int32_t n,
                                  const int32_t* pos, const int32_t* coords, const int32_t* slots, void* stream);
 
+/* Bytes of workspace that fd_token_attend_device needs for these sizes (weights: 1 if
+ * weight_out will be given). Host only. */
+fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, int32_t n, int32_t weights,
+                                    size_t* bytes);
+
+/* Attention of n new tokens per request over the cache (GQA as in Sec. 3.2: head h
+ * reads group h / (heads / groups)). For request b, token i, head h, over the slots s
+ * of its group that it sees -- pos[s] >= 0 and, if causal, pos[s] <= pos[b][i] --
+ *   x_s = scale q . K[s],  p = softmax(x),  out = sum_s p_s V[s],  lse = log sum_s exp x_s,
+ *   weight_out[s] = decay weight[s] + sum over the group's heads and tokens of p_s
+ * (0 for empty slots). Tokens with pos < 0 are padding and see nothing; a row that sees
+ * nothing gives out 0 and lse -infinity and adds nothing to the weights. Nothing
+ * that a row does not see reaches its results, infinities and NaN included. A decoder's
+ * frame mask is causal = 1 with the frame index as every token's position.
+ *   q, out      [batch][n][heads][head_dim] of the cache's dtype by strides (host arrays:
+ *               batch, token, head; whole 16 bytes), rows 16-byte aligned, no overlap
+ *   lse         [batch][heads][n] fp32, or NULL
+ *   weight_out  [batch][groups][capacity], may be the cache's weight, or NULL: not
+ *               computed
+ *   workspace   16-byte aligned, at least fd_token_attend_workspace bytes; its contents
+ *               mean nothing between calls. Calls that may overlap, and captured graphs
+ *               that may be replayed at once, need one each.
+ * scale finite and > 0, decay finite. Scores, softmax statistics, output sums and weights
+ * are fp32; for 16-bit caches the probabilities enter P V rounded to that type (for
+ * few rows as a sum of two such values). Results do not change from run to run. n x heads / groups <= 2^24,
+ * batch x n x heads <= 2^28, batch x groups x capacity <= 2^31, else UNSUPPORTED. */
+fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, const int64_t q_stride[3], int32_t heads,
+                                 int32_t n, const int32_t* pos, float scale, int32_t causal, void* out,
+                                 const int64_t out_stride[3], float* lse, float decay, float* weight_out,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
 const char* fd_status_string(fd_status status);
 
 /* Message of the last failed call on this thread ("" if none). */

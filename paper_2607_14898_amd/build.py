@@ -15,7 +15,8 @@ ROOT = os.path.dirname(PKG)
 SOURCES = ["csrc/k_gemm_f16.hip", "csrc/k_gemm_bf16.hip", "csrc/k_gemm_fp8.hip",
            "csrc/k_gemm_f32.hip", "csrc/k_gemm.hip",
            "csrc/k_attn.hip", "csrc/k_misc.hip", "csrc/k_probe.hip", "csrc/fd_scratch.hip",
-           "csrc/k_rope.hip", "csrc/k_slots.hip", "csrc/fd_token.cpp", "csrc/fd_runtime.cpp"]
+           "csrc/k_rope.hip", "csrc/k_slots.hip", "csrc/k_token_attn.hip",
+           "csrc/fd_token.cpp", "csrc/fd_runtime.cpp"]
 LIB = os.path.join(PKG, "libflashdecoder.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

@@ -219,4 +219,71 @@ fd_status fd_token_append_device(const fd_token_cache* cache, const fd_rope* rop
   return launched(fd::token_append(c, r, a, kind_of(cache->dtype), (hipStream_t)stream), "append");
 }
 
+// Sizes of an attention call that the launches can index.
+static fd_status check_attend(const fd::TokenCacheArgs& c, int32_t heads, int32_t n) {
+  if (heads < 1 || heads % c.G) return fail(FD_ERR_INVALID_ARGUMENT, "heads %d must be a multiple of groups %d", heads, c.G);
+  if (n < 0) return fail(FD_ERR_INVALID_ARGUMENT, "n must be >= 0");
+  const int64_t rows = (int64_t)n * (heads / c.G), bg = (int64_t)c.B * c.G;
+  if (rows > (int64_t)1 << 24 || bg * rows > (int64_t)1 << 28 || bg * c.C > (int64_t)1 << 31)
+    return fail(FD_ERR_UNSUPPORTED,
+                "n x heads / groups above 2^24, batch x n x heads above 2^28, or batch x groups x capacity above 2^31");
+  return FD_OK;
+}
+
+fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, int32_t n, int32_t weights,
+                                    size_t* bytes) {
+  fd::TokenCacheArgs c;
+  fd_status st = check_cache(cache, &c);
+  if (st != FD_OK) return st;
+  if ((st = check_attend(c, heads, n)) != FD_OK) return st;
+  if (!bytes) return fail(FD_ERR_INVALID_ARGUMENT, "NULL pointer");
+  *bytes = n == 0 ? 0 : (size_t)fd::token_attend_plan(c, n, heads / c.G, kind_of(cache->dtype), weights != 0).bytes;
+  return FD_OK;
+}
+
+fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, const int64_t q_stride[3], int32_t heads,
+                                 int32_t n, const int32_t* pos, float scale, int32_t causal, void* out,
+                                 const int64_t out_stride[3], float* lse, float decay, float* weight_out,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  fd::TokenCacheArgs c;
+  fd_status st = check_cache(cache, &c);
+  if (st != FD_OK) return st;
+  if ((st = check_attend(c, heads, n)) != FD_OK) return st;
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(FD_ERR_INVALID_ARGUMENT, "scale must be finite and > 0");
+  if (!std::isfinite(decay)) return fail(FD_ERR_INVALID_ARGUMENT, "decay must be finite");
+  if ((uintptr_t)weight_out % 4 || (uintptr_t)lse % 4)
+    return fail(FD_ERR_INVALID_ARGUMENT, "lse and weight_out must be 4-byte aligned");
+  const int kind = kind_of(cache->dtype), rep = heads / c.G;
+  fd::TokenAttend a;
+  a.n = n;
+  a.rep = rep;
+  a.scale = scale;
+  a.causal = causal != 0;
+  a.lse = lse;
+  a.weight_out = weight_out;
+  a.decay = decay;
+  if (n > 0) {
+    if (!q || !out || !q_stride || !out_stride || !pos) return fail(FD_ERR_INVALID_ARGUMENT, "NULL pointer");
+    const int es = elem_size(cache->dtype);
+    const auto extents = {(int64_t)c.B, (int64_t)n, (int64_t)heads};
+    if (((uintptr_t)q | (uintptr_t)out) % 16 || (uintptr_t)pos % 4)
+      return fail(FD_ERR_INVALID_ARGUMENT, "q and out must be 16-byte aligned, pos 4-byte aligned");
+    if (!strides_ok(q_stride, extents, c.D, es) || !strides_ok(out_stride, extents, c.D, es))
+      return fail(FD_ERR_INVALID_ARGUMENT, "strides of q and out must be at least head_dim and whole 16 bytes");
+    const int64_t need = fd::token_attend_plan(c, n, rep, kind, weight_out != nullptr).bytes;
+    if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (size_t)need))
+      return fail(FD_ERR_INVALID_ARGUMENT, "workspace of %zu bytes, %lld needed (16-byte aligned)", workspace_bytes,
+                  (long long)need);
+    a.q = q;
+    a.out = out;
+    for (int i = 0; i < 3; ++i) {
+      a.qs[i] = q_stride[i];
+      a.os[i] = out_stride[i];
+    }
+    a.pos = pos;
+    a.ws = workspace;
+  }
+  return launched(fd::token_attend(c, a, kind, (hipStream_t)stream), "token attention");
+}
+
 }  // extern "C"

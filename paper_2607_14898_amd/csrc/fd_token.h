@@ -63,4 +63,34 @@ struct TokenSlots {
 constexpr int kMaxSlotTokens = 65536;  // new tokens of one choice
 hipError_t token_slots(const TokenSlots& a, hipStream_t stream);
 
+// Attention over a token cache. Row r = i rep + h of a (request, group) is query
+// token i of the group's head h (R = n rep rows), so that a tile of rows covers
+// neighbouring tokens of every head that shares the keys.
+struct TokenAttend {
+  const void* q = nullptr;     // [B][n][N][D] by strides (batch, token, head)
+  void* out = nullptr;
+  int64_t qs[3] = {}, os[3] = {};
+  const int* pos = nullptr;    // [B][n], < 0: padding
+  int n = 0, rep = 1;
+  float scale = 1.f;
+  int causal = 1;
+  float* lse = nullptr;        // [B][N][n] or null
+  float* weight_out = nullptr; // [B][G][C] or null
+  float decay = 1.f;
+  void* ws = nullptr;          // token_attend_plan().bytes
+};
+
+// How a call is laid out, from its sizes alone.
+struct TokenAttendPlan {
+  int by_keys = 0;      // few rows: waves share a row tile and part the keys
+  int row_tiles = 1;    // tiles of 32 rows (by_keys) or 128
+  int splits = 1;       // parts of the slots
+  int weight_parts = 1; // parts of the rows in the pass over the weights
+  // offsets into the workspace, in floats
+  int64_t part_o = 0, part_ml = 0, lse2 = 0, scores = 0, weights = 0;
+  int64_t bytes = 0;
+};
+TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int kind, bool weights);
+hipError_t token_attend(const TokenCacheArgs& c, const TokenAttend& a, int kind, hipStream_t stream);
+
 }  // namespace fd

@@ -119,6 +119,8 @@ def load_library() -> ctypes.CDLL:
         "fd_rope_device": (I32, [P, P, I32, I64, I32, I32, I64, I64, P, P, I64, I64, P]),
         "fd_token_slots_device": (I32, [P, P, I32, I32, I32, P, I32, I32, I32, P, P]),
         "fd_token_append_device": (I32, [P, P, P, P, P, P, I32, P, P, P, P]),
+        "fd_token_attend_workspace": (I32, [P, I32, I32, I32, ctypes.POINTER(SZ)]),
+        "fd_token_attend_device": (I32, [P, P, P, I32, I32, P, ctypes.c_float, I32, P, P, P, ctypes.c_float, P, P, SZ, P]),
         "fd_status_string": (ctypes.c_char_p, [I32]),
         "fd_last_error": (ctypes.c_char_p, []),
     }
@@ -638,6 +640,7 @@ class TokenCache:
         self._s = fd_token_cache(ctypes.sizeof(fd_token_cache), dt, B, G, C, D, k.data_ptr(), v.data_ptr(),
                                  I3(*k.stride()[:3]), I3(*v.stride()[:3]), pos.data_ptr(), weight.data_ptr())
         self._p = ctypes.addressof(self._s)
+        self._ws = {}
 
     @classmethod
     def empty(cls, batch: int, groups: int, capacity: int, head_dim: int, dtype, device="cuda") -> "TokenCache":
@@ -684,3 +687,37 @@ class TokenCache:
         slots = self.choose(pos, keep_first, keep_recent, stream)
         self.append(k, v, pos, slots, rope, coords, stream)
         return slots
+
+    def attend(self, q, pos, scale: Optional[float] = None, causal: bool = True, track: bool = True,
+               decay: float = 1.0, weight_out=None, out=None, stream=None):
+        """Attention of q [batch, n, heads, head_dim] at pos [batch, n] over the cache
+        (fd_token_attend_device); scale defaults to head_dim ** -0.5. Returns (out, lse
+        [batch, heads, n]). With track the slots' weights become decay x weight + what
+        they received, in place or in weight_out."""
+        import torch
+        B, n, heads, D = q.shape
+        dev = self.pos.device
+        _need(q, "q", self.k.dtype, (self.batch, n, heads, self.head_dim), dev, strided=True)
+        _need(pos, "pos", torch.int32, (B, n), dev)
+        if weight_out is not None:
+            _need(weight_out, "weight_out", torch.float32, self.weight.shape, dev)
+        elif track:
+            weight_out = self.weight
+        if out is None:
+            out = _new(q.shape, q.dtype, dev, stream)
+        else:
+            _need(out, "out", q.dtype, q.shape, dev, strided=True)
+        lse = _new((B, heads, n), torch.float32, dev, stream)
+        lib, I3 = load_library(), ctypes.c_int64 * 3
+        key = (heads, n, weight_out is not None)
+        size = self._ws.get(key)
+        if size is None:  # (a number that follows from the sizes; the memory is each call's own)
+            b = ctypes.c_size_t()
+            _check(lib.fd_token_attend_workspace(self._p, heads, n, int(key[2]), ctypes.byref(b)))
+            size = self._ws[key] = b.value
+        ws = _new((size,), torch.uint8, dev, stream)
+        _call_on(dev, stream, lib.fd_token_attend_device, self._p, q.data_ptr(), I3(*q.stride()[:3]), heads, n,
+                 pos.data_ptr(), D ** -0.5 if scale is None else scale, int(causal), out.data_ptr(),
+                 I3(*out.stride()[:3]), lse.data_ptr(), decay,
+                 None if weight_out is None else weight_out.data_ptr(), ws.data_ptr(), size)
+        return out, lse

@@ -1,0 +1,326 @@
+"""Attention over a token cache on the GPU against a plain implementation in 64 bits:
+outputs, log-sums and the slots' weights, and a stream that inserts and attends."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_14898_amd import flashdecoder as fdb
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+
+
+def ref(k, v, at, weight, q, pos, scale, causal, decay):
+    """(out, lse, weight) in 64 bits, and bounds on the error of the library's arithmetic."""
+    B, G, C, D = k.shape
+    n, N = q.shape[1], q.shape[2]
+    h = N // G
+    bits = q.dtype
+    half = torch.finfo(bits).eps / 2
+    k, v, q = (t.cpu().double() for t in (k, v, q))
+    at, pos, weight = at.cpu(), pos.cpu(), weight.cpu().double()
+    out = torch.zeros(B, n, N, D, dtype=torch.float64)
+    lse = torch.full((B, N, n), -math.inf, dtype=torch.float64)
+    w = torch.where(at >= 0, decay * weight, 0.0)
+    t_out, t_lse, t_w = torch.zeros_like(out), torch.zeros_like(lse), 2.0 ** -23 * w.abs()
+    u = 2.0 ** -24
+    for b in range(B):
+        for head in range(N):
+            g = head // h
+            for i in range(n):
+                if pos[b, i] < 0:
+                    continue
+                see = at[b, g] >= 0
+                if causal:
+                    see &= at[b, g] <= pos[b, i]
+                if not see.any():
+                    continue
+                kk, vv = k[b, g, see], v[b, g, see]
+                x = scale * (kk @ q[b, i, head])
+                lse[b, head, i] = torch.logsumexp(x, 0)
+                p = torch.softmax(x, 0)
+                o = p @ vv
+                out[b, i, head] = o
+                w[b, g, see] += p
+                # scores: D products summed in fp32, three roundings of the scaled score, one of the log-sum it is
+                # taken from; exp2 and log2 within two steps; sums over the slots in fp32
+                ex = ((D + 3) * u * scale * (kk.abs() @ q[b, i, head].abs())).max() + 4 * u * (x.abs().max() + 8)
+                rel = 2 * ex + (len(x) + 16) * u
+                # probabilities go into P V rounded to 16 bits (fp16 below 2^-31 of the row's largest as nothing)
+                sharp = half if bits != F32 else u
+                spread = p @ vv.abs()
+                t_out[b, i, head] = spread * (rel + sharp) + len(x) * 2.0 ** -31 * vv.abs().max() + half * o.abs() \
+                    + torch.finfo(bits).tiny
+                t_lse[b, head, i] = ex + (len(x) + 8) * u + 4 * u * lse[b, head, i].abs()
+                t_w[b, g, see] += p * (rel + 4 * u) + 4 * u * p
+    t_w += n * h * u * w.abs()
+    return (out, lse, w), (t_out, t_lse, t_w)
+
+
+def near(got, want, tol):
+    got = got.cpu().double()
+    inf = torch.isinf(want)
+    assert torch.equal(got[inf], want[inf])
+    bad = ~((got - want).abs() <= tol)[~inf]
+    assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} off, most {(got - want)[~inf].abs().max():.3e}"
+
+
+def make(B, G, N, D, n, C, dtype, seed=0, fill=1.0, unit=1, pad=0, sharp=1.0):
+    """Random cache with new tokens at the largest positions, empty slots of NaN, padding behind and between."""
+    r = np.random.default_rng(seed)
+    gen = torch.Generator().manual_seed(seed)
+    k, v = (torch.randn(B, G, C, D, generator=gen).to(dtype) for _ in range(2))
+    q = (sharp * torch.randn(B, n, N, D, generator=gen)).to(dtype)
+    used = max(min(n, C), int(round(fill * C)))
+    at = np.full((B, G, C), -1, np.int32)
+    for b in range(B):
+        for g in range(G):
+            s = r.permutation(C)[:used]
+            at[b, g, s] = r.permutation(2 * used)[:used] // unit
+    at = torch.from_numpy(at)
+    pos = torch.from_numpy(np.sort(r.integers(0, 2 * used, (B, n)), 1).astype(np.int32)) // unit
+    for b in range(B):
+        if pad:
+            pos[b, n - pad:] = -1
+            pos[b, : n : 5] = -1
+    k[at < 0] = float("nan")
+    v[at < 0] = float("inf")
+    weight = torch.rand(B, G, C, generator=gen)
+    weight[at < 0] = float("nan")
+    return tuple(t.cuda() for t in (k, v, at, weight, q, pos))
+
+
+def check(k, v, at, weight, q, pos, causal=True, scale=None, decay=1.0):
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    cache = fdb.TokenCache(k, v, at, weight)
+    w_out = torch.full_like(weight, float("nan"))
+    before = weight.clone()
+    out, lse = cache.attend(q, pos, scale=scale, causal=causal, decay=decay, weight_out=w_out)
+    want, tol = ref(k, v, at, weight, q, pos, np.float64(np.float32(scale)), causal, float(np.float32(decay)))
+    near(out, want[0], tol[0])
+    near(lse, want[1], tol[1])
+    near(w_out, want[2], tol[2])
+    assert torch.equal(weight.nan_to_num(7.0), before.nan_to_num(7.0))
+    # without weights (other launches): the same up to the same bounds; run again: the same bits
+    out2, lse2 = cache.attend(q, pos, scale=scale, causal=causal, track=False)
+    near(out2, want[0], tol[0])
+    near(lse2, want[1], tol[1])
+    again = torch.empty_like(w_out)
+    out3, lse3 = cache.attend(q, pos, scale=scale, causal=causal, decay=decay, weight_out=again)
+    assert torch.equal(out3, out) and torch.equal(lse3, lse) and torch.equal(again, w_out)
+    return out, lse, w_out
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("B,G,N,n,C,fill", [
+    (1, 1, 1, 1, 1, 1.0), (2, 2, 8, 1, 33, 0.7), (1, 2, 6, 1, 1000, 1.0), (2, 1, 7, 5, 257, 0.4), (1, 1, 32, 2, 700, 1.0),
+    (1, 1, 3, 22, 130, 1.0), (1, 2, 2, 129, 190, 0.9), (1, 1, 4, 65, 1100, 1.0)])
+def test_attend(dtype, D, B, G, N, n, C, fill):
+    for causal in (True, False):
+        check(*make(B, G, N, D, n, C, dtype, seed=D + C, fill=fill, unit=1 + C % 3), causal=causal, decay=0.75)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n", [1, 9, 70])
+def test_padding_and_rows_that_see_nothing(dtype, n):
+    k, v, at, weight, q, pos = make(2, 2, 4, 64, n, 150, dtype, seed=n, pad=min(n, 3))
+    q[pos < 0] = float("nan")  # padding holds anything
+    pos[1, n // 2] = 0
+    at[1, at[1] == 0] = 1      # ... nothing lies at or before position 0
+    check(k, v, at, weight, q, pos)
+    # an empty cache, a request of padding alone
+    at.fill_(-3)
+    out, lse, w = check(k, v, at, weight, q, pos)
+    assert not out.any() and bool((lse == -math.inf).all()) and not w.any()
+    pos.fill_(-1)
+    check(*make(2, 2, 4, 64, n, 150, dtype)[:4], q, pos)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n", [4, 60])
+def test_infinities_and_nan_that_some_rows_do_not_see(dtype, n):
+    """Slots later than some rows hold NaN, infinities and the type's largest values."""
+    k, v, at, weight, q, pos = make(1, 2, 6, 64, n, 200, dtype, seed=3, fill=0.9)
+    # the later half of the tokens sees everything, the earlier half nothing at positions from `edge` on
+    edge = int(at.max()) // 2
+    pos[:, : n // 2] = edge - 1
+    pos[:, n // 2:] = int(at.max()) + 1
+    early = (pos[0] < edge).cpu()
+    hidden = at >= edge
+    fine = [t.clone() for t in (k, v)]
+    for bad in (float("nan"), float("inf"), -float("inf"), torch.finfo(dtype).max):
+        k2, v2 = k.clone(), v.clone()
+        k2[hidden], v2[hidden] = bad, bad
+        cache = fdb.TokenCache(k2, v2, at, weight)
+        out, lse = cache.attend(q, pos, track=False)
+        want, tol = ref(*fine, at, weight, q, pos, 64 ** -0.5, True, 1.0)
+        near(out[:, early], want[0][:, early], tol[0][:, early])
+        near(lse[:, :, early], want[1][:, :, early], tol[1][:, :, early])
+    # values alone: a row that sees +inf in a dim has +inf there, both signs or NaN give NaN, other dims are exact
+    late = ~early
+    some = hidden.nonzero()[:2].tolist()
+    v2 = v.clone()
+    (b0, g0, s0), (_, _, s1) = some[0], [x for x in hidden.nonzero().tolist() if x[:2] == some[0][:2]][1]
+    v2[b0, g0, s0, 5] = float("inf")
+    v2[b0, g0, s0, 40] = float("inf")
+    v2[b0, g0, s1, 40] = -float("inf")
+    v2[b0, g0, s1, 63] = float("nan")
+    out, _ = fdb.TokenCache(k, v2, at, weight).attend(q, pos, track=False)
+    want, tol = ref(*fine, at, weight, q, pos, 64 ** -0.5, True, 1.0)
+    near(out[:, early], want[0][:, early], tol[0][:, early])
+    heads = slice(3 * g0, 3 * g0 + 3)
+    got = out[0, late][:, heads].cpu().double()
+    assert bool((got[..., 5] == math.inf).all()) and bool(got[..., [40, 63]].isnan().all())
+    plain = [d for d in range(64) if d not in (5, 40, 63)]
+    near(got[..., plain], want[0][0, late][:, heads][..., plain], tol[0][0, late][:, heads][..., plain])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n", [1, 40])
+def test_scores_far_apart(dtype, n):
+    """Logits that rise steeply along the slots, all far below zero, and far above."""
+    for shift in (0.0, -150.0, 150.0):
+        k, v, at, weight, q, pos = make(1, 1, 3, 64, n, 600, dtype, seed=5)
+        k[..., 0] = (torch.arange(600) / 600.0 * 40 + shift).to(dtype)
+        q[..., 0] = 8.0
+        q[..., 1:] *= 0.1
+        check(k, v, at, weight, q, pos, causal=False)
+
+
+def test_strides():
+    """Rows of larger buffers, heads before tokens, and what lies beside them left as it was."""
+    for dtype, n in ((F16, 2), (BF16, 75), (F32, 75)):
+        k, v, at, weight, q, pos = make(2, 2, 4, 64, n, 170, dtype, seed=9, fill=0.8)
+        plain = fdb.TokenCache(k, v, at, weight).attend(q, pos, weight_out=torch.empty_like(weight))
+        kb = torch.full((2, 171, 3, 96), 5.0, device="cuda").to(dtype)
+        vb = torch.full((3, 2, 170, 64), 5.0, device="cuda").to(dtype)
+        kv, vv = kb[:, 1:, 1:, 16:80].transpose(1, 2), vb[1:]
+        kv.copy_(k), vv.copy_(v)
+        qb = torch.full((2, 4, n + 1, 80), 3.0, device="cuda").to(dtype)
+        ob = torch.full((2, 4, n + 2, 80), 3.0, device="cuda").to(dtype)
+        qv, ov = qb[:, :, 1:, 8:72].transpose(1, 2), ob[:, :, 1:-1, 8:72].transpose(1, 2)
+        qv.copy_(q)
+        out, lse = fdb.TokenCache(kv, vv, at, weight).attend(qv, pos, out=ov, weight_out=torch.empty_like(weight))
+        assert out is ov and torch.equal(ov, plain[0]) and torch.equal(lse, plain[1])
+        ov.fill_(3.0)
+        assert bool((ob == 3.0).all())
+
+
+@pytest.mark.parametrize("n", [1, 64])
+def test_far_slots(n):
+    """Slots 2^20 elements apart: the last ones lie beyond 2^31 elements and 2^32 bytes."""
+    C, D, step = 2100, 64, 2 ** 20
+    big = torch.empty(C * step, dtype=F16, device="cuda")
+    k, v, at, weight, q, pos = make(1, 1, 2, D, n, C, F16, seed=11)
+    far_k, far_v = (torch.as_strided(big, (1, 1, C, D), (C * step, C * step, step, 1), o) for o in (0, 64))
+    far_k.copy_(k), far_v.copy_(v)
+    a, b = (fdb.TokenCache(x, y, at, weight).attend(q, pos, weight_out=torch.empty_like(weight))
+            for x, y in ((far_k, far_v), (k, v)))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    cache = fdb.TokenCache(far_k, far_v, at, weight)
+    slots = torch.tensor([[[C - 1]]], dtype=torch.int32, device="cuda")
+    new = torch.randn(1, 1, 1, D, device="cuda").half()
+    cache.append(new, -new, pos[:, :1].contiguous(), slots)
+    assert torch.equal(far_k[0, 0, C - 1], new[0, 0, 0]) and torch.equal(far_v[0, 0, C - 1], -new[0, 0, 0])
+    assert torch.equal(far_k[0, 0, : C - 1], k[0, 0, : C - 1])
+
+
+def test_no_tokens():
+    k, v, at, weight, q, pos = make(1, 2, 4, 64, 3, 50, F16, fill=0.5)
+    cache = fdb.TokenCache(k, v, at, weight)
+    out, lse = cache.attend(q[:, :0], pos[:, :0].contiguous(), decay=0.5)
+    want = torch.where(at >= 0, 0.5 * make(1, 2, 4, 64, 3, 50, F16, fill=0.5)[3], 0.0)
+    assert out.shape == (1, 0, 4, 64) and torch.equal(cache.weight, want)
+
+
+@pytest.mark.parametrize("n", [1, 80])
+def test_captured_and_side_streams(n):
+    """Two captured graphs replayed in turn with eager calls between, and a call on another stream."""
+    sets = [make(2, 2, 4, 64, n, 900, BF16, seed=s) for s in (1, 2)]
+    caches = [fdb.TokenCache(*s[:4]) for s in sets]
+    wouts = [torch.zeros_like(s[3]) for s in sets]
+    eager = [c.attend(s[4], s[5], weight_out=w) for c, s, w in zip(caches, sets, wouts)]
+    eager = [(o.clone(), l.clone(), w.clone()) for (o, l), w in zip(eager, wouts)]
+    graphs, outs = [], []
+    for c, s, w in zip(caches, sets, wouts):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.attend(s[4], s[5], weight_out=w))
+        graphs.append(g)
+    for _ in range(3):
+        for w in wouts:
+            w.fill_(-1.0)
+        for g in graphs:
+            g.replay()
+        caches[0].attend(sets[0][4], sets[0][5], track=False)
+        torch.cuda.synchronize()
+        for (o, l), w, e in zip(outs, wouts, eager):
+            assert torch.equal(o, e[0]) and torch.equal(l, e[1]) and torch.equal(w, e[2])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [c.attend(s[4], s[5], weight_out=w, stream=side) for c, s, w in zip(caches, sets, wouts)]
+    side.synchronize()
+    for (o, l), w, e in zip(got, wouts, eager):
+        assert torch.equal(o, e[0]) and torch.equal(l, e[1]) and torch.equal(w, e[2])
+
+
+def test_frame_mask_of_the_decoder():
+    """Frame indices as positions give the decoder's mask: a frame's tokens see each other and earlier frames."""
+    L, frames = 30, 3
+    k, v, at, weight, q, pos = make(1, 1, 4, 64, L, L * frames, F16, seed=4)
+    at.copy_((torch.arange(L * frames) // L).view(1, 1, -1))
+    pos.fill_(1)
+    out, lse, w = check(k, v, at, weight, q, pos)
+    half = fdb.TokenCache(k[:, :, : 2 * L].contiguous(), v[:, :, : 2 * L].contiguous(), at[:, :, : 2 * L].contiguous(),
+                          weight[:, :, : 2 * L].contiguous())
+    want, tol = ref(half.k, half.v, half.pos, half.weight, q, pos, 64 ** -0.5, False, 1.0)
+    near(out, want[0], tol[0])
+    assert torch.equal(w[:, :, 2 * L:], weight[:, :, 2 * L:])
+
+
+@pytest.mark.parametrize("dtype", [F16, F32])
+def test_stream(dtype):
+    """Tokens in chunks through insert and attend, against a cache of Python lists."""
+    B, G, N, D, C = 2, 2, 6, 64, 48
+    gen = torch.Generator().manual_seed(0)
+    freq, mag = fdb.fd_rope_frequencies(32, scaling="linear", factor=2.0)
+    rope = fdb.Rope(freq, layout="half", magnitude=mag)
+    cache = fdb.TokenCache.empty(B, G, C, D, dtype)
+    t = 0
+    for step, n in enumerate([40, 1, 1, 12, 1, 30, 1]):
+        k, v, q = (torch.randn(B, n, h, D, generator=gen).to(dtype).cuda() for h in (G, G, N))
+        pos = (t + torch.arange(n, dtype=torch.int32)).expand(B, n).clone()
+        if n > 10:
+            pos[1, n - 4:] = -1
+        pos = pos.cuda()
+        t += n
+        old = [x.cpu().clone() for x in (cache.k, cache.v, cache.pos, cache.weight)]
+        slots = cache.insert(k, v, pos, rope=rope, keep_first=4, keep_recent=8)
+        qr = rope(q.reshape(B * n, N, D), pos.clamp(min=0).reshape(-1)).view(B, n, N, D)
+        kr = rope(k.reshape(B * n, G, D), pos.clamp(min=0).reshape(-1)).view(B, n, G, D).cpu()
+        # the rule, slot by slot
+        for b in range(B):
+            new = [i for i in range(n) if int(pos[b, i]) >= 0]
+            newest = max(int(pos[b, i]) for i in new)
+            for g in range(G):
+                kind = lambda s: (lambda p: 0 if p < 0 else 3 if p < 4 else 2 if p > newest - 8 else 1)(int(old[2][b, g, s]))  # noqa: E731
+                order = sorted(range(C), key=lambda s: (kind(s), float(old[3][b, g, s]) if kind(s) else 0.0, s))
+                for i, s in zip(new, sorted(order[: len(new)])):
+                    assert int(slots[b, g, i]) == s
+                    old[0][b, g, s], old[1][b, g, s] = kr[b, i, g], v[b, i, g].cpu()
+                    old[2][b, g, s], old[3][b, g, s] = int(pos[b, i]), 0.0
+        for got, want in zip((cache.k, cache.v, cache.pos, cache.weight), old):
+            assert torch.equal(got.cpu(), want)
+        want, tol = ref(*(x.cuda() for x in old), qr, pos, D ** -0.5, True, float(np.float32(0.9)))
+        out, lse = cache.attend(qr, pos, decay=0.9)
+        near(out, want[0], tol[0])
+        near(lse, want[1], tol[1])
+        near(cache.weight, want[2], tol[2])
+    assert bool((cache.pos >= 0).all())
+    cache.reset()
+    out, lse = cache.attend(qr, pos)
+    assert not out.any() and not cache.weight.any()

@@ -146,6 +146,40 @@ def test_append_refusals():
     assert _append_call(lib, n=0, k=None, slots=None) == fdb.FD_OK
 
 
+def _attend_call(lib, cache=None, q=A, qs=(1024, 256, 64), heads=4, n=3, pos=A, scale=0.125, causal=1, out=A,
+                 os_=(1024, 256, 64), lse=A, decay=1.0, w=A, ws=A, size=1 << 40):
+    I3 = ctypes.c_int64 * 3
+    c = cache_struct() if cache is None else cache
+    return lib.fd_token_attend_device(ctypes.byref(c), q, I3(*qs) if qs else None, heads, n, pos, scale, causal, out,
+                                      I3(*os_) if os_ else None, lse, decay, w, ws, size, None)
+
+
+def test_attend_refusals():
+    lib = _lib()
+    size = ctypes.c_size_t()
+    for kw, status in BAD_CACHES:
+        assert _attend_call(lib, cache_struct(**kw)) == status, kw
+        assert lib.fd_token_attend_workspace(ctypes.byref(cache_struct(**kw)), 4, 3, 1, ctypes.byref(size)) == status
+    c = cache_struct()
+    assert lib.fd_token_attend_workspace(ctypes.byref(c), 4, 3, 1, None) == INVALID
+    assert lib.fd_token_attend_workspace(ctypes.byref(c), 3, 3, 1, ctypes.byref(size)) == INVALID
+    assert lib.fd_token_attend_workspace(ctypes.byref(c), 4, 0, 1, ctypes.byref(size)) == fdb.FD_OK and size.value == 0
+    assert lib.fd_token_attend_workspace(ctypes.byref(c), 4, 3, 1, ctypes.byref(size)) == fdb.FD_OK and size.value > 0
+    need = size.value
+    for kw in (dict(heads=0), dict(heads=3), dict(heads=-2), dict(n=-1), dict(q=None), dict(out=None), dict(pos=None),
+               dict(qs=None), dict(os_=None), dict(q=A + 8), dict(out=A + 2), dict(pos=A + 1), dict(lse=A + 2),
+               dict(w=A + 1), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan),
+               dict(decay=math.inf), dict(decay=math.nan), dict(qs=(1024, 256, 60)), dict(qs=(1024, 0, 64)),
+               dict(os_=(1024, 250, 64)), dict(ws=None), dict(ws=A + 8), dict(size=need - 1), dict(size=0)):
+        assert _attend_call(lib, **kw) == INVALID, kw
+    for kw in (dict(heads=4, n=1 << 24), dict(heads=2 << 20, n=64)):
+        assert _attend_call(lib, **kw) == UNSUPPORTED, kw
+    huge = cache_struct(batch=300, groups=200, capacity=1 << 20, k_stride=(1 << 40, 1 << 30, 64),
+                        v_stride=(1 << 40, 1 << 30, 64))
+    assert _attend_call(lib, huge, heads=200) == UNSUPPORTED
+    assert _attend_call(lib, n=0, q=None, ws=None, w=None) in (fdb.FD_OK, fdb.FD_ERR_DEVICE)  # nothing to launch
+
+
 def test_binding_refusals():
     """Wrong tensors are refused before anything reaches the library."""
     _lib()
