@@ -492,7 +492,7 @@ typedef struct fd_token_cache {
   void* k;                /* [batch][groups][capacity][head_dim] by strides      */
   void* v;
   int64_t k_stride[3];    /* batch, group, slot, in elements: whole 16 bytes and */
-  int64_t v_stride[3];    /*   at least head_dim                                 */
+  int64_t v_stride[3];    /*   at least head_dim; slots below 2^24 bytes apart   */
   int32_t* pos;           /* [batch][groups][capacity], < 0: empty               */
   float* weight;          /* [batch][groups][capacity], accumulated attention    */
 } fd_token_cache;
@@ -546,8 +546,9 @@ fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, 
  *               that may be replayed at once, need one each.
  * scale finite and > 0, decay finite. Scores, softmax statistics, output sums and weights
  * are fp32; for 16-bit caches the probabilities enter P V rounded to that type (for
- * few rows as a sum of two such values). Results do not change from run to run. n x heads / groups <= 2^24,
- * batch x n x heads <= 2^28, batch x groups x capacity <= 2^31, else UNSUPPORTED. */
+ * few rows as a sum of two such values). Results do not change from run to run.
+ * heads / groups <= 256, n x heads / groups <= 2^24, batch x n x heads <= 2^28, batch x
+ * groups x capacity <= 2^31, else UNSUPPORTED. */
 fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, const int64_t q_stride[3], int32_t heads,
                                  int32_t n, const int32_t* pos, float scale, int32_t causal, void* out,
                                  const int64_t out_stride[3], float* lse, float decay, float* weight_out,

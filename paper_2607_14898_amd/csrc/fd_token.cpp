@@ -69,6 +69,8 @@ fd_status check_cache(const fd_token_cache* c, fd::TokenCacheArgs* a) {
   const auto extents = {(int64_t)c->batch, (int64_t)c->groups, (int64_t)c->capacity};
   if (!strides_ok(c->k_stride, extents, c->head_dim, es) || !strides_ok(c->v_stride, extents, c->head_dim, es))
     return fail(FD_ERR_INVALID_ARGUMENT, "cache strides must be at least head_dim and whole 16 bytes");
+  if (c->capacity > 1 && (c->k_stride[2] * es >= 1 << 24 || c->v_stride[2] * es >= 1 << 24))
+    return fail(FD_ERR_UNSUPPORTED, "slot strides must be below 2^24 bytes");
   a->k = c->k;
   a->v = c->v;
   a->pos = c->pos;
@@ -224,6 +226,7 @@ static fd_status check_attend(const fd::TokenCacheArgs& c, int32_t heads, int32_
   if (heads < 1 || heads % c.G) return fail(FD_ERR_INVALID_ARGUMENT, "heads %d must be a multiple of groups %d", heads, c.G);
   if (n < 0) return fail(FD_ERR_INVALID_ARGUMENT, "n must be >= 0");
   const int64_t rows = (int64_t)n * (heads / c.G), bg = (int64_t)c.B * c.G;
+  if (heads / c.G > 256) return fail(FD_ERR_UNSUPPORTED, "more than 256 heads a group");
   if (rows > (int64_t)1 << 24 || bg * rows > (int64_t)1 << 28 || bg * c.C > (int64_t)1 << 31)
     return fail(FD_ERR_UNSUPPORTED,
                 "n x heads / groups above 2^24, batch x n x heads above 2^28, or batch x groups x capacity above 2^31");

@@ -72,6 +72,7 @@ struct TokenAttend {
   int64_t qs[3] = {}, os[3] = {};
   const int* pos = nullptr;    // [B][n], < 0: padding
   int n = 0, rep = 1;
+  uint32_t rep_inv = 0;        // ceil(2^32 / rep), set by the launcher
   float scale = 1.f;
   int causal = 1;
   float* lse = nullptr;        // [B][N][n] or null
@@ -85,6 +86,7 @@ struct TokenAttendPlan {
   int by_keys = 0;      // few rows: waves share a row tile and part the keys
   int row_tiles = 1;    // tiles of 32 rows (by_keys) or 128
   int splits = 1;       // parts of the slots
+  int scan = 1;         // slots that a workgroup sorts at a time (not by_keys)
   int weight_parts = 1; // parts of the rows in the pass over the weights
   // offsets into the workspace, in floats
   int64_t part_o = 0, part_ml = 0, lse2 = 0, scores = 0, weights = 0;

@@ -156,16 +156,28 @@ template <typename T> __device__ __forceinline__ u32x4 finite_part(u32x4 x) {
   return w.u;
 }
 
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, bytes, 0x00020000);
+}
+__device__ __forceinline__ uint32_t lds_address(const u32x4* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const u32x4*)p;
+}
+
 // The rows of a call: where a row's query lies, and the first position it does not see.
 struct Row {
   int i, head;     // query token, head
   uint32_t lim;
 };
+// r / rep: below 2^24 and for rep <= 256 the high word of r ceil(2^32 / rep) is exact
+// (the multiplier is less than rep / 2^32 too large, and r rep < 2^32).
+__device__ __forceinline__ int token_of(const TokenAttend& a, int r) {
+  return a.rep == 1 ? r : (int)__umulhi((uint32_t)r, a.rep_inv);
+}
 __device__ __forceinline__ Row row_of(const TokenAttend& a, int b, int g, int64_t r, int64_t R) {
   Row w{0, g * a.rep, 0};
   if (r < R) {
-    w.i = (int)(r / a.rep);
-    w.head = g * a.rep + (int)(r - (int64_t)w.i * a.rep);
+    w.i = token_of(a, (int)r);
+    w.head = g * a.rep + (int)r - w.i * a.rep;
     const int p = a.pos[(int64_t)b * a.n + w.i];
     w.lim = p < 0 ? 0u : a.causal ? (uint32_t)p + 1u : 0x80000000u;
   }
@@ -213,28 +225,41 @@ template <typename T, int D, bool EXACT> struct Softmax {
         for (int r = 0; r < 16; ++r) acc[d][r] *= f;
     }
     const float sub = m == -INFINITY ? 0.f : O::kShift - m;
+    // 16 keys at a time where registers are short, else all the exponentials before all
+    // the MFMAs (which then run at raised priority in one go)
+    constexpr int NX = KB * 2, GX = D == 128 ? 1 : NX;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int x0 = 0; x0 < NX; x0 += GX) {
+      // (V's fragments are on their way while the exponentials are taken)
+      typename O::V ph[GX], pl[GX], vf[GX][D / 32];
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        typename O::V ph, pl;
+      for (int y = 0; y < GX; ++y)
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) vf[y][d] = Tile<T, D>::v_frag(vt, row0 + 16 * (x0 + y), d, lane);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int y = 0; y < GX; ++y)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][8 * st + e], c, sub));
+          const int x = x0 + y;
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[x / 2][8 * (x % 2) + e], c, sub));
           l += p;
           // P enters the second MFMA in the cache's type. Where memory bounds the kernel
           // (EXACT) what that rounding loses goes in by a second MFMA; elsewhere its half
           // step per key, as large as the output's own rounding, is kept.
-          ph[e] = (T)p;
-          if constexpr (EXACT && sizeof(T) == 2) pl[e] = (T)(p - (float)ph[e]);
+          ph[y][e] = (T)p;
+          if constexpr (EXACT && sizeof(T) == 2) pl[y][e] = (T)(p - (float)ph[y][e]);
         }
+      __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+      for (int y = 0; y < GX; ++y)
 #pragma unroll
         for (int d = 0; d < D / 32; ++d) {
-          const typename O::V vf = Tile<T, D>::v_frag(vt, row0 + 32 * kb + 16 * st, d, lane);
-          acc[d] = O::mma(vf, ph, acc[d]);
-          if constexpr (EXACT && sizeof(T) == 2) acc[d] = O::mma(vf, pl, acc[d]);
+          acc[d] = O::mma(vf[y][d], ph[y], acc[d]);
+          if constexpr (EXACT && sizeof(T) == 2) acc[d] = O::mma(vf[y][d], pl[y], acc[d]);
         }
-      }
+      __builtin_amdgcn_s_setprio(0);
+    }
   }
   __device__ __forceinline__ bool finite() const {
     float t = 0.f;
@@ -300,23 +325,28 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   const T* kb = (const T*)c.k + b * c.ks[0] + g * c.ks[1];
   const T* vb = (const T*)c.v + b * c.vs[0] + g * c.vs[1];
   const int* ps = c.pos + (int64_t)bg * c.C;
-  float* score = a.weight_out ? (float*)a.ws + pl.scores + ((int64_t)bg * R + row) * c.C : nullptr;
 
   const int tiles = (c.C + 31) / 32, per = (tiles + pl.splits - 1) / pl.splits;
   const int t0 = split * per + wave, t1 = min(tiles, (split + 1) * per);
-  auto pos_at = [&](int t) {
-    const int s = t * 32 + lr;
-    return t < t1 && s < c.C ? ps[s] : -1;
-  };
   u32x4* tile = buf[wave];
   Softmax<T, D, true> sx;
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
-    int p_next = pos_at(t0);
-    for (int t = t0; t < t1; t += 4) {
-      const int p = p_next;
-      p_next = pos_at(t + 4);
-      if ((uint32_t)__ballot((uint32_t)p < lim_max) == 0) continue;
+    for (int tc = t0; tc < t1; tc += 4 * 64) {
+      // which of the wave's next 64 tiles any row sees, two tiles a load: walked one by one,
+      // an empty tile would cost a wait for memory
+      uint64_t live = 0;
+#pragma unroll 8
+      for (int x = 0; x < 32; ++x) {
+        const int t = tc + 4 * (2 * x + lh), sp = t * 32 + lr;
+        const uint64_t m = __ballot((t < t1 && sp < c.C ? (uint32_t)ps[sp] : ~0u) < lim_max);
+        live |= (uint64_t)((uint32_t)m != 0) << (2 * x) | (uint64_t)((uint32_t)(m >> 32) != 0) << (2 * x + 1);
+        if (tc + 8 * (x + 1) >= t1) break;
+      }
+      while (live) {
+      const int t = tc + 4 * __builtin_ctzll(live);
+      live &= live - 1;
+      const int p = t * 32 + lr < c.C ? ps[t * 32 + lr] : -1;
       const uint32_t taken = (uint32_t)__ballot(p >= 0);
       const bool all = (uint32_t)__ballot((uint32_t)p < lim_min) == ~0u;
       u32x4 kr[NV], vr[NV];
@@ -341,13 +371,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
       for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) s[0] = Op<T>::mma(TL::k_frag(tile, key_of_row(lr), ks, lh), qf[ks], s[0]);
-      if (score && row < R) {
-        const int s0 = t * 32 + 8 * lh;
+      if (a.weight_out && row < R) {  // [tile][row][32]: whole lines, however few the rows
+        float* score = (float*)a.ws + pl.scores + (((int64_t)bg * tiles + t) * R + row) * 32 + 8 * lh;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int sl_ = s0 + 16 * (r >> 3) + (r & 7);
-          if (sl_ < c.C) score[sl_] = s[0][r];
-        }
+        for (int r = 0; r < 16; r += 4)
+          store4(score + 16 * (r >> 3) + (r & 4), s[0][r], s[0][r + 1], s[0][r + 2], s[0][r + 3]);
       }
       if (!all) {
 #pragma unroll
@@ -372,6 +400,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
       __builtin_amdgcn_wave_barrier();
       __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      }
     }
     if (scrub || __ballot(w.lim != 0 && !sx.finite()) == 0) {
       if (scrub)
@@ -451,6 +480,13 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
 // Many rows (a chunk of tokens): the matrix cores and the exponentials bound it. A
 // workgroup's four waves own 32 rows each and share tiles of KT slots through LDS, two
 // of them in turn: the next tile's 16-byte loads fly while a tile is computed.
+//
+// Slots are taken through a list. In a cache that has turned over, a chunk's own tokens
+// lie scattered among the old ones and every tile of consecutive slots would need a mask,
+// so the workgroup first sorts kScan slots' indices by what its rows see of them: those
+// that all rows see, those that some see (the chunk's own tokens, later ones left out),
+// nothing else. Only the second kind is masked, and empty slots cost no tile.
+constexpr int kScan = 4096;
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
@@ -458,8 +494,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   constexpr int NV = KT * TL::CPR / 256;
   __shared__ u32x4 sk[2][KT * TL::CPR], sv[2][KT * TL::CPR];
   __shared__ int spos[2][KT];
-  __shared__ uint32_t slim[4];
-  __shared__ uint32_t slive[4];
+  __shared__ uint16_t list[kScan];
+  __shared__ uint32_t slim[2][4];
+  __shared__ int scount[2][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   // Workgroups are dealt to the 8 XCDs in turn; each XCD takes a contiguous range of
@@ -473,7 +510,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   const int64_t row = (int64_t)rt * 128 + wave * 32 + lr;
   const Row w = row_of(a, b, g, row, R);
   const uint32_t lim_max = lanes_max(w.lim), lim_min = lanes_min(w.lim ? w.lim : ~0u);
-  if (lane == 0) slim[wave] = lim_max;
+  if (lane == 0) {
+    slim[0][wave] = lim_max;
+    slim[1][wave] = lim_min;
+  }
   const float cs = a.scale * kLog2e;
   typename Op<T>::V qf[D / 16];
   {
@@ -489,80 +529,132 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   const T* vbase = (const T*)c.v + b * c.vs[0] + g * c.vs[1];
   const int* ps = c.pos + (int64_t)bg * c.C;
   __syncthreads();
-  const uint32_t wg_lim = max(max(slim[0], slim[1]), max(slim[2], slim[3]));
+  const uint32_t wg_lim = max(max(slim[0][0], slim[0][1]), max(slim[0][2], slim[0][3]));
+  const uint32_t wg_min = min(wg_lim, min(min(slim[1][0], slim[1][1]), min(slim[1][2], slim[1][3])));
 
-  const int tiles = (c.C + KT - 1) / KT, per = (tiles + pl.splits - 1) / pl.splits;
-  const int t_lo = split * per, t_hi = min(tiles, t_lo + per);
-  u32x4 kr[NV], vr[NV];
+  const int per = (c.C + pl.splits - 1) / pl.splits;
+  const int s_lo = split * per, s_hi = min(c.C, s_lo + per);
+  const uint32_t kstep = (uint32_t)c.ks[2] * sizeof(T), vstep = (uint32_t)c.vs[2] * sizeof(T);  // below 2^24
+  const uint32_t lds_k = lds_address(&sk[0][0]), lds_v = lds_address(&sv[0][0]);
+  auto pos_of = [&](int s) { return *(const int*)((const char*)ps + 4u * (uint32_t)s); };
   int pr = -1;
-  auto load = [&](int t) __attribute__((always_inline)) {
+  int c0 = 0, m = 0, seen = 0;  // the scanned range's first slot, its list's length, those that all rows see
+  __amdgpu_buffer_rsrc_t rk, rv;
+  // Tile t goes to LDS by DMA, 16 bytes a lane in lane order, so the lane picks the chunk
+  // that belongs where it writes (both permutations are their own inverses).
+  auto load = [&](int t, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int idx = j * 256 + tid, kr_ = idx / TL::CPR, ch = idx % TL::CPR;
-      const int64_t s = min(t * KT + kr_, c.C - 1);
-      kr[j] = *reinterpret_cast<const u32x4*>(kbase + s * c.ks[2] + ch * TL::EPC);
-      vr[j] = *reinterpret_cast<const u32x4*>(vbase + s * c.vs[2] + ch * TL::EPC);
+      const int idx = j * 256 + tid, r = idx / TL::CPR, e = t * KT + r;
+      const uint32_t s = list[min(e, m - 1)];
+      const uint32_t ok = __umul24(s, kstep) + 16 * (TL::k(r, idx % TL::CPR) - r * TL::CPR);
+      const uint32_t ov = __umul24(s, vstep) + 16 * (TL::v(r, idx % TL::CPR) - r * TL::CPR);
+      const uint32_t at = 16u * (uint32_t)(buf * KT * TL::CPR + j * 256 + wave * 64);
+      // M0 is reserved by the compiler, but nothing else in this kernel reads it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_k + at), "v"(ok), "s"(rk) : "m0");
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_v + at), "v"(ov), "s"(rv) : "m0");
+#pragma clang diagnostic pop
     }
-    const int s = t * KT + lane;
-    pr = (KT == 64 || lane < KT) && s < c.C ? ps[s] : -1;
+    if ((t + 1) * KT > seen && tid < KT) {
+      const int e = t * KT + tid;
+      pr = e < m ? pos_of(c0 + list[e]) : -1;
+    }
   };
-  auto stage = [&](int buf, bool scrub) __attribute__((always_inline)) {
-    const uint64_t taken = __ballot(pr >= 0);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int idx = j * 256 + tid, r = idx / TL::CPR, ch = idx % TL::CPR;
-      u32x4 x = vr[j];
-      if (!(taken >> r & 1)) x = u32x4{0, 0, 0, 0};
-      if (scrub) x = finite_part<T>(x);
-      sk[buf][TL::k(r, ch)] = kr[j];
-      sv[buf][TL::v(r, ch)] = x;
+  // the DMA of tile t is complete and its readers may begin, those of the one before are done
+  auto arrive = [&](int t, int buf, bool scrub) __attribute__((always_inline)) {
+    if ((t + 1) * KT > seen && tid < KT) spos[buf][tid] = pr;
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (scrub) {
+#pragma unroll 1
+      for (int idx = tid; idx < KT * TL::CPR; idx += 256) sv[buf][idx] = finite_part<T>(sv[buf][idx]);
+      __syncthreads();
     }
-    if (tid < KT) spos[buf][tid] = pr;
   };
 
   Softmax<T, D, false> sx;
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
-    for (int c0 = t_lo; c0 < t_hi; c0 += 64) {
-      // which of the next 64 tiles any row of the workgroup sees: 16 tiles a wave
-      uint32_t mine = 0;
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        const int t = c0 + wave * 16 + x, s = t * KT + lane;
-        const int p = t < t_hi && (KT == 64 || lane < KT) && s < c.C ? ps[s] : -1;
-        mine |= __ballot((uint32_t)p < wg_lim) ? 1u << x : 0u;
-      }
-      __syncthreads();  // the last tiles' readers are done, and slive's
-      if (lane == 0) slive[wave] = mine;
-      __syncthreads();
-      uint64_t live = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) live |= (uint64_t)__builtin_amdgcn_readfirstlane(slive[x]) << (16 * x);
-      if (live == 0) continue;
-      auto next = [&]() __attribute__((always_inline)) {
-        const int x = __builtin_ctzll(live);
-        live &= live - 1;
-        return c0 + x;
+    for (c0 = s_lo; c0 < s_hi; c0 += pl.scan) {
+      const int c1 = min(s_hi, c0 + pl.scan);
+      auto scanned = [&](int x) {
+        const int s = c0 + wave * (kScan / 4) + x * 64 + lane;
+        return (uint32_t)(s < c1 ? pos_of(s) : -1);
       };
-      load(next());
-      stage(0, scrub);
+      int n0 = 0, n1 = 0;
+#pragma unroll 8
+      for (int x = 0; x < kScan / 256; ++x) {
+        const uint32_t p = scanned(x);
+        n0 += (int)__popcll(__ballot(p < wg_min));
+        n1 += (int)__popcll(__ballot(p - wg_min < wg_lim - wg_min));
+      }
+      __syncthreads();  // the last range's readers are done
+      if (lane == 0) {
+        scount[0][wave] = n0;
+        scount[1][wave] = n1;
+      }
       __syncthreads();
-      for (int cur = 0;; cur ^= 1) {
-        const bool more = live != 0;
-        if (more) load(next());
-        const int p = spos[cur][lane % KT];
-        if (__ballot((uint32_t)p < lim_max) != 0) {
-          const bool all = __ballot((uint32_t)p < lim_min) == ~0ull;
+      seen = scount[0][0] + scount[0][1] + scount[0][2] + scount[0][3];
+      m = seen + scount[1][0] + scount[1][1] + scount[1][2] + scount[1][3];
+      if (m == 0) continue;
+      int at0 = 0, at1 = seen;
+      for (int x = 0; x < wave; ++x) {
+        at0 += scount[0][x];
+        at1 += scount[1][x];
+      }
+      const uint64_t below = (1ull << lane) - 1;
+#pragma unroll 8
+      for (int x = 0; x < kScan / 256; ++x) {
+        const uint32_t p = scanned(x);
+        const bool k0 = p < wg_min, k1 = p - wg_min < wg_lim - wg_min;
+        const uint64_t b0 = __ballot(k0), b1 = __ballot(k1);
+        const uint16_t s = (uint16_t)(wave * (kScan / 4) + x * 64 + lane);
+        if (k0) list[at0 + (int)__popcll(b0 & below)] = s;
+        if (k1) list[at1 + (int)__popcll(b1 & below)] = s;
+        at0 += (int)__popcll(b0);
+        at1 += (int)__popcll(b1);
+      }
+      __syncthreads();
+      seen = __builtin_amdgcn_readfirstlane(seen);
+      m = __builtin_amdgcn_readfirstlane(m);
+      rk = buffer_of(kbase + (int64_t)c0 * c.ks[2], (uint32_t)(c1 - c0 - 1) * kstep + D * (uint32_t)sizeof(T));
+      rv = buffer_of(vbase + (int64_t)c0 * c.vs[2], (uint32_t)(c1 - c0 - 1) * vstep + D * (uint32_t)sizeof(T));
+      const int tiles = (m + KT - 1) / KT;
+      load(0, 0);
+      arrive(0, 0, scrub);
+      for (int t = 0; t < tiles; ++t) {
+        const int cur = t & 1;
+        if (t + 1 < tiles) load(t + 1, cur ^ 1);
+        bool any = lim_max != 0, all = true;
+        if ((t + 1) * KT > seen) {
+          const int q = spos[cur][lane % KT];
+          any = __ballot((uint32_t)q < lim_max) != 0;
+          all = __ballot((uint32_t)q < lim_min) == ~0ull;
+        }
+        if (any) {
           f32x16 s[KB];
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+          // (a wave at its MFMAs issues them ahead of the other waves on the SIMD, whose
+          // exponentials fill in between: 10% at 64 dims, 1% at 128)
+          __builtin_amdgcn_s_setprio(3);
+          typename Op<T>::V kf[D / 16][KB];
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-              s[kb] = Op<T>::mma(TL::k_frag(sk[cur], 32 * kb + key_of_row(lr), ks, lh), qf[ks], s[kb]);
+            for (int kb = 0; kb < KB; ++kb) kf[ks][kb] = TL::k_frag(sk[cur], 32 * kb + key_of_row(lr), ks, lh);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[ks][kb], qf[ks], s[kb]);
+          __builtin_amdgcn_s_setprio(0);
           if (!all) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -572,14 +664,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
           }
           sx.template add<KB>(s, cs, sv[cur], 0, lane);
         }
-        if (!more) break;
-        stage(cur ^ 1, scrub);
-        __syncthreads();
+        if (t + 1 < tiles) arrive(t + 1, cur ^ 1, scrub);
       }
     }
     __syncthreads();
     if (scrub) {
-      for (int x = t_lo * KT; x < min(t_hi * KT, c.C); ++x)
+      for (int x = s_lo; x < s_hi; ++x)
         if ((uint32_t)ps[x] < w.lim) sx.add_unbounded(vbase + x * c.vs[2], lh);
       break;
     }
@@ -591,13 +681,20 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     sx.l = 0.f;
   }
   const float L = other_half_sum(sx.l);
-  if (row >= R) return;
+  // (the row's place is worked out again, from a lane the compiler takes for another:
+  // kept through the loop it would cost registers that 128 dims do not have)
+  int lane_ = lane;
+  asm volatile("" : "+v"(lane_));
+  const int64_t row_ = (int64_t)rt * 128 + wave * 32 + (lane_ & 31);
+  const int lh_ = lane_ >> 5;
+  if (row_ >= R) return;
+  const Row w_ = row_of(a, b, g, row_, R);
   const bool none = sx.m == -INFINITY;
   const float l2 = none ? -INFINITY : sx.m - Op<T>::kShift + __builtin_amdgcn_logf(L);
   if (pl.splits > 1) {
-    const int64_t pr_ = ((int64_t)bg * pl.splits + split) * R + row;
+    const int64_t pr_ = ((int64_t)bg * pl.splits + split) * R + row_;
     float* ml = (float*)a.ws + pl.part_ml + pr_ * 2;
-    if (lh == 0) {
+    if (lh_ == 0) {
       ml[0] = sx.m;
       ml[1] = L;
     }
@@ -606,15 +703,15 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        store4(o + 32 * d + 2 * r + 4 * lh, sx.acc[d][r], sx.acc[d][r + 1], sx.acc[d][r + 2], sx.acc[d][r + 3]);
+        store4(o + 32 * d + 2 * r + 4 * lh_, sx.acc[d][r], sx.acc[d][r + 1], sx.acc[d][r + 2], sx.acc[d][r + 3]);
     return;
   }
-  if (lh == 0) {
-    if (a.weight_out) ((float*)a.ws)[pl.lse2 + (int64_t)bg * R + row] = l2;
-    if (a.lse) a.lse[((int64_t)b * c.G * a.rep + w.head) * a.n + w.i] = none ? -INFINITY : l2 * kLn2;
+  if (lh_ == 0) {
+    if (a.weight_out) ((float*)a.ws)[pl.lse2 + (int64_t)bg * R + row_] = l2;
+    if (a.lse) a.lse[((int64_t)b * c.G * a.rep + w_.head) * a.n + w_.i] = none ? -INFINITY : l2 * kLn2;
   }
   const float inv = none ? 0.f : 1.f / L;
-  T* o = out_of<T>(a, b, w);
+  T* o = out_of<T>(a, b, w_);
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -622,63 +719,82 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
       float x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : sx.acc[d][r + e] * inv;
-      store4(o + 32 * d + 2 * r + 4 * lh, x[0], x[1], x[2], x[3]);
+      store4(o + 32 * d + 2 * r + 4 * lh_, x[0], x[1], x[2], x[3]);
     }
 }
 
 // What is left when the parts are done: workgroups below row_blocks join the parts of
-// rows (D / 4 threads each), the others add up what rows gave 256 slots each, from the
-// scores that attend_keys_kernel kept (4 bytes a row and slot, beside 4 D of a 16-bit key
-// and value). Each of those works out its rows' log-sums from the parts by itself.
+// rows (D / 4 threads each), the others add up what rows gave kFinishSlots slots each,
+// from the scores that attend_keys_kernel kept (4 bytes a row and slot, beside 4 D of a
+// 16-bit key and value). Each of those works out its rows' log-sums from the parts by
+// itself, 16 threads a row. Parts are read side by side throughout: a chain of dependent
+// loads per part cost 0.7 us each.
+// Four slots a thread once that still leaves two workgroups a CU.
 constexpr int kFinishRows = 64;
-template <typename T, int D>
+template <typename T, int D, int NS>
 __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl,
                                                      int row_blocks, int slot_blocks) {
   __shared__ float s_l2[kFinishRows];
   __shared__ uint32_t s_lim[kFinishRows];
   const float* ws = (const float*)a.ws;
-  const int64_t R = (int64_t)a.n * a.rep;
+  const int R = a.n * a.rep;
   const int S = pl.splits;
   const int tid = threadIdx.x;
-  // shift and sum of row r of (b, g) over the parts
-  auto total = [&](int64_t bg, int64_t r, float& M, float& L) {
+  // shift and sum of row r of (b, g) over the parts, by W neighbouring threads (j: this one's place)
+  auto total = [&](int64_t bg, int r, int j, auto width, float& M, float& L) {
+    constexpr int W = decltype(width)::value;
+    const float2* ml = reinterpret_cast<const float2*>(ws + pl.part_ml) + bg * S * R + r;
     M = -INFINITY;
     L = 0.f;
-    for (int s = 0; s < S; ++s) M = fmaxf(M, ws[pl.part_ml + ((bg * S + s) * R + r) * 2]);
-    if (M == -INFINITY) return;
-    for (int s = 0; s < S; ++s) {
-      const float2 ml = *reinterpret_cast<const float2*>(ws + pl.part_ml + ((bg * S + s) * R + r) * 2);
-      if (ml.x != -INFINITY) L += ml.y * __builtin_amdgcn_exp2f(ml.x - M);
+    for (int s = j; s < S; s += W) {
+      const float2 x = ml[(int64_t)s * R];
+      const float m = fmaxf(M, x.x);
+      if (m != -INFINITY) L = L * __builtin_amdgcn_exp2f(M - m) + x.y * __builtin_amdgcn_exp2f(x.x - m);
+      M = m;
+    }
+#pragma unroll
+    for (int o = 1; o < W; o <<= 1) {
+      const float M2 = __shfl_xor(M, o), L2 = __shfl_xor(L, o), m = fmaxf(M, M2);
+      if (m != -INFINITY) {
+        // (the lower lane's share first, so that all of them round alike)
+        const float x = L * __builtin_amdgcn_exp2f(M - m), y = L2 * __builtin_amdgcn_exp2f(M2 - m);
+        L = j & o ? y + x : x + y;
+      }
+      M = m;
     }
   };
   if ((int)blockIdx.x < row_blocks) {
     constexpr int TPR = D / 4, RPB = 256 / TPR;
-    const int64_t x = (int64_t)blockIdx.x * RPB + tid / TPR;  // row over all (b, g)
-    const int d = 4 * (tid % TPR);
-    if (x >= (int64_t)c.B * c.G * R) return;
-    const int64_t bg = x / R, r = x - bg * R;
+    const int64_t rows = (int64_t)c.B * c.G * R;
+    const int64_t x_ = (int64_t)blockIdx.x * RPB + tid / TPR, x = min(x_, rows - 1);  // row over all (b, g)
+    const int j = tid % TPR, d = 4 * j;
+    const int64_t bg = x / R;
+    const int r = (int)(x - bg * R);
     const int b = (int)(bg / c.G), g = (int)(bg - (int64_t)b * c.G);
     float M, L;
-    total(bg, r, M, L);
+    total(bg, r, j, std::integral_constant<int, TPR>{}, M, L);
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (M != -INFINITY) {
-      for (int s = 0; s < S; ++s) {
-        const int64_t pr = (bg * S + s) * R + r;
-        const float ms = ws[pl.part_ml + pr * 2];
-        if (ms == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(ms - M);
-        const float4 p = *reinterpret_cast<const float4*>(ws + pl.part_o + pr * D + d);
-        o.x += f * p.x;
-        o.y += f * p.y;
-        o.z += f * p.z;
-        o.w += f * p.w;
+    const float* po = ws + pl.part_o + (bg * S * R + r) * D + d;
+    const float2* ml = reinterpret_cast<const float2*>(ws + pl.part_ml) + bg * S * R + r;
+#pragma unroll 4
+    for (int s = 0; s < S; ++s) {
+      const float ms = ml[(int64_t)s * R].x;
+      const float4 p = *reinterpret_cast<const float4*>(po + (int64_t)s * R * D);
+      const float f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
+      if (f != 0.f) {  // (a part that saw nothing holds no number)
+        o.x = fmaf(f, p.x, o.x);
+        o.y = fmaf(f, p.y, o.y);
+        o.z = fmaf(f, p.z, o.z);
+        o.w = fmaf(f, p.w, o.w);
       }
-      const float inv = 1.f / L;
-      o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     }
+    if (x_ >= rows) return;
     const Row w = row_of(a, b, g, r, R);
+    if (M == -INFINITY) o = make_float4(0.f, 0.f, 0.f, 0.f);
+    else o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     store4(out_of<T>(a, b, w) + d, o.x, o.y, o.z, o.w);
-    if (d == 0) {
+    if (j == 0) {
       const float l2 = M == -INFINITY ? -INFINITY : M - Op<T>::kShift + __builtin_amdgcn_logf(L);
       if (a.weight_out && !pl.by_keys) ((float*)a.ws)[pl.lse2 + x] = l2;
       if (a.lse) a.lse[((int64_t)b * c.G * a.rep + w.head) * a.n + w.i] = M == -INFINITY ? -INFINITY : l2 * kLn2;
@@ -688,76 +804,141 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
   const int y = blockIdx.x - row_blocks;
   const int64_t bg = y / slot_blocks;
   const int b = (int)(bg / c.G), g = (int)(bg - (int64_t)b * c.G);
-  const int s = (y % slot_blocks) * 256 + tid;
-  const int p = s < c.C ? c.pos[bg * c.C + s] : -1;
-  float sum = 0.f;
+  const int s0 = (y % slot_blocks) * 256 * NS + tid;
+  const int tiles = (c.C + 31) / 32;
+  uint32_t p[NS];
+  float sum[NS];
+#pragma unroll
+  for (int x = 0; x < NS; ++x) {
+    p[x] = s0 + 256 * x < c.C ? (uint32_t)c.pos[bg * c.C + s0 + 256 * x] : ~0u;
+    sum[x] = 0.f;
+  }
   const float cs = a.scale * kLog2e;
-  for (int64_t r0 = 0; r0 < R; r0 += kFinishRows) {
-    const int m = (int)min((int64_t)kFinishRows, R - r0);
+  for (int r0 = 0; r0 < R; r0 += kFinishRows) {
+    const int m = min(kFinishRows, R - r0);
     __syncthreads();
-    if (tid < m) {
+    for (int q = tid / 16; q < (m + 15) / 16 * 16; q += 16) {
       float M, L;
-      total(bg, r0 + tid, M, L);
-      s_l2[tid] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
-      s_lim[tid] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + tid, R).lim;
+      total(bg, r0 + min(q, m - 1), tid % 16, std::integral_constant<int, 16>{}, M, L);
+      if (tid % 16 == 0 && q < m) {
+        s_l2[q] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
+        s_lim[q] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + q, R).lim;
+      }
     }
     __syncthreads();
-    if (p >= 0)
-      for (int r = 0; r < m; ++r)
-        if ((uint32_t)p < s_lim[r])
-          sum += __builtin_amdgcn_exp2f(fmaf(ws[pl.scores + (bg * R + r0 + r) * c.C + s], cs, -s_l2[r]));
+    const float* sc[NS];
+#pragma unroll
+    for (int x = 0; x < NS; ++x) {
+      const int s = min(s0 + 256 * x, c.C - 1);
+      sc[x] = ws + pl.scores + ((bg * tiles + s / 32) * R + r0) * 32 + s % 32;
+    }
+    for (int r = 0; r < m; r += 4) {
+      float v[NS][4];  // (of tiles that no row sees, whatever the workspace held: not used)
+#pragma unroll
+      for (int x = 0; x < NS; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[x][e] = sc[x][min(r + e, m - 1) * 32];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lim = r + e < m ? s_lim[min(r + e, m - 1)] : 0u;
+        const float l2 = s_l2[min(r + e, m - 1)];
+#pragma unroll
+        for (int x = 0; x < NS; ++x)
+          if (p[x] < lim) sum[x] += __builtin_amdgcn_exp2f(fmaf(v[x][e], cs, -l2));
+      }
+    }
   }
-  if (s < c.C) {
-    const int64_t at = bg * c.C + s;
-    a.weight_out[at] = p < 0 ? 0.f : fmaf(a.decay, c.weight[at], sum);
-  }
+#pragma unroll
+  for (int x = 0; x < NS; ++x)
+    if (s0 + 256 * x < c.C) {
+      const int64_t at = bg * c.C + s0 + 256 * x;
+      a.weight_out[at] = p[x] >= 0x80000000u ? 0.f : fmaf(a.decay, c.weight[at], sum[x]);
+    }
 }
 
 // The weights of a chunk of tokens: p = exp2(score - lse) needs the rows' log-sums, so
 // the scores are computed again, with the keys held and the rows streaming past: a wave
-// keeps 32 KB keys' fragments in registers and the four waves share tiles of 32 rows
-// through LDS. Half the matrix work of the attention, and its exponentials.
+// keeps 32 KB keys' fragments in registers and the four waves share tiles of 64 rows
+// through LDS. Half the matrix work of the attention, and its exponentials. A
+// workgroup's slots are taken in the order seen by every row, by some rows, empty, so
+// that a mask costs the waves with the call's own tokens alone.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
   constexpr int KB = sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
-  constexpr int NV = (32 * TL::CPR + 255) / 256;
-  __shared__ u32x4 sq[2][32 * TL::CPR];
-  __shared__ float sl2[2][32];
-  __shared__ uint32_t slim[2][32];
+  constexpr int KW = 128 * KB;                // slots of a workgroup
+  constexpr int RT = 64;                      // rows of a tile
+  constexpr int NV = RT * TL::CPR / 256;
+  __shared__ u32x4 sq[2][RT * TL::CPR];
+  __shared__ float sl2[2][RT];
+  __shared__ uint32_t slim[2][RT];
+  __shared__ int lslot[KW];       // the workgroup's slots in that order
+  __shared__ uint32_t lpos[KW];   // and their positions (empty: from 2^31 on)
+  __shared__ uint32_t smin;
+  __shared__ int scount[3][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  const int slot_blocks = (c.C + 128 * KB - 1) / (128 * KB);
+  const int slot_blocks = (c.C + KW - 1) / KW;
   const int kbk = blockIdx.x % slot_blocks, part = blockIdx.x / slot_blocks;
   const int bg = blockIdx.y, b = bg / c.G, g = bg - b * c.G;
   const int64_t R = (int64_t)a.n * a.rep;
-  const int s0 = kbk * 128 * KB + wave * 32 * KB;
-  const int* ps = c.pos + (int64_t)bg * c.C;
   const T* kbase = (const T*)c.k + b * c.ks[0] + g * c.ks[1];
+  const T* qbase = (const T*)a.q + b * a.qs[0] + g * a.rep * a.qs[2];
   const float* l2 = (const float*)a.ws + pl.lse2 + (int64_t)bg * R;
   const float cs = a.scale * kLog2e;
+  const int64_t row_tiles = (R + RT - 1) / RT, per = (row_tiles + pl.weight_parts - 1) / pl.weight_parts;
+  const int64_t t0 = part * per, t1 = min(row_tiles, t0 + per);
+
+  // the first position that some row of this part does not see
+  if (tid == 0) smin = ~0u;
+  __syncthreads();
+  if (t0 < t1) {
+    uint32_t lim = ~0u;
+    const int i1 = token_of(a, (int)min(R, t1 * RT) - 1);
+    for (int i = token_of(a, (int)(t0 * RT)) + tid; i <= i1; i += 256) {
+      const uint32_t l = row_of(a, b, g, (int64_t)i * a.rep, R).lim;
+      lim = l ? min(lim, l) : lim;
+    }
+    lim = lanes_min(lim);
+    if (lane == 0) atomicMin(&smin, lim);
+  }
+  __syncthreads();
+  {
+    const int s = kbk * KW + tid;
+    const uint32_t p = tid < KW && s < c.C ? (uint32_t)c.pos[(int64_t)bg * c.C + s] : ~0u;
+    const int cls = p < smin ? 0 : p < 0x80000000u ? 1 : 2;
+    uint64_t m[3];
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+      m[x] = __ballot(cls == x);
+      if (lane == 0) scount[x][wave] = (int)__popcll(m[x]);
+    }
+    __syncthreads();
+    int at = (int)__popcll(m[cls] & ((1ull << lane) - 1));
+    for (int x = 0; x <= cls; ++x)
+      for (int w = 0; w < (x < cls ? 4 : wave); ++w) at += scount[x][w];
+    if (at < KW) {  // (threads beyond the slots come last)
+      lslot[at] = min(s, c.C - 1);
+      lpos[at] = p;
+    }
+  }
+  __syncthreads();
 
   typename Op<T>::V kf[KB][D / 16];
-  int kp[KB][16];          // positions of the lane's 16 keys a block (register r: key 8 (r / 4) + 4 lh + r % 4)
   uint32_t p_max = 0, p_min = ~0u;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
-    const T* k = kbase + (int64_t)min(s0 + 32 * kb + lr, c.C - 1) * c.ks[2];
+    const int at = (wave * KB + kb) * 32 + lr;
+    const uint32_t p = lpos[at];
+    p_max = p < 0x80000000u ? max(p_max, p) : p_max;  // (what empty slots add up is not stored)
+    p_min = min(p_min, p);
+    const T* k = kbase + (int64_t)lslot[at] * c.ks[2];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) kf[kb][ks] = *reinterpret_cast<const typename Op<T>::V*>(k + 16 * ks + 8 * lh);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int s = s0 + 32 * kb + 8 * (r >> 2) + 4 * lh + (r & 3);
-      kp[kb][r] = s < c.C ? ps[s] : -1;
-      p_max = max(p_max, (uint32_t)kp[kb][r]);
-      p_min = min(p_min, (uint32_t)kp[kb][r]);
-    }
   }
-  p_max = lanes_max(p_max);  // an empty slot among them: >= 2^31, so that no row sees them all
+  p_max = lanes_max(p_max);
   p_min = lanes_min(p_min);
 
-  const int64_t row_tiles = (R + 31) / 32, per = (row_tiles + pl.weight_parts - 1) / pl.weight_parts;
-  const int64_t t0 = part * per, t1 = min(row_tiles, t0 + per);
   u32x4 qr[NV];
   float l2r = 0.f;
   uint32_t limr = 0;
@@ -765,15 +946,11 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int idx = j * 256 + tid, ch = idx % TL::CPR;
-      if (32 * TL::CPR % 256 == 0 || idx < 32 * TL::CPR) {
-        const int64_t r = min(t * 32 + idx / TL::CPR, R - 1);
-        const int i = (int)(r / a.rep);
-        qr[j] = *reinterpret_cast<const u32x4*>((const T*)a.q + b * a.qs[0] + i * a.qs[1] +
-                                                (g * a.rep + (int)(r - (int64_t)i * a.rep)) * a.qs[2] + ch * TL::EPC);
-      }
+      const int r = min((int)t * RT + idx / TL::CPR, (int)R - 1), i = token_of(a, r);
+      qr[j] = *reinterpret_cast<const u32x4*>(qbase + i * a.qs[1] + (r - i * a.rep) * a.qs[2] + ch * TL::EPC);
     }
-    if (tid < 32) {
-      const int64_t r = t * 32 + tid;
+    if (tid < RT) {
+      const int64_t r = t * RT + tid;
       l2r = r < R ? l2[r] : 0.f;
       limr = r < R && l2r != -INFINITY ? row_of(a, b, g, r, R).lim : 0u;
     }
@@ -782,9 +959,9 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int idx = j * 256 + tid;
-      if (32 * TL::CPR % 256 == 0 || idx < 32 * TL::CPR) sq[buf][TL::k(idx / TL::CPR, idx % TL::CPR)] = qr[j];
+      sq[buf][TL::k(idx / TL::CPR, idx % TL::CPR)] = qr[j];
     }
-    if (tid < 32) {
+    if (tid < RT) {
       sl2[buf][tid] = l2r;
       slim[buf][tid] = limr;
     }
@@ -802,28 +979,42 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
   for (int64_t t = t0; t < t1; ++t) {
     const int cur = (int)(t - t0) & 1;
     if (t + 1 < t1) load(t + 1);
-    const uint32_t lim = slim[cur][lr];
-    if (__ballot(lim > p_min) != 0) {
+#pragma unroll
+    for (int rb = 0; rb < RT / 32; ++rb) {
+      const uint32_t lim = slim[cur][32 * rb + lr];
+      if (__ballot(lim > p_min) == 0) continue;
       const bool all = __ballot(lim > p_max) == ~0ull;
-      const float nl = -sl2[cur][lr];
+      const float nl = -sl2[cur][32 * rb + lr];
       f32x16 s[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+      // (all fragments are on their way before the first MFMA: left to itself the compiler
+      // waits for each of them in turn)
+      typename Op<T>::V q[D / 16];
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const typename Op<T>::V q = TL::k_frag(sq[cur], lr, ks, lh);
+      for (int ks = 0; ks < D / 16; ++ks) q[ks] = TL::k_frag(sq[cur], 32 * rb + lr, ks, lh);
+      if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[kb][ks], q, s[kb]);
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[kb][ks], q[ks], s[kb]);
+      if (all) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[kb][r] += __builtin_amdgcn_exp2f(fmaf(s[kb][r], cs, nl));
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const uint32_t p = lpos[(wave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)];
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[kb][r], cs, nl));
+            sum[kb][r] += p < lim ? x : 0.f;
+          }
       }
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], cs, nl));
-          sum[kb][r] += all || (uint32_t)kp[kb][r] < lim ? p : 0.f;
-        }
     }
     if (t + 1 < t1) stage(cur ^ 1);
     __syncthreads();
@@ -836,11 +1027,12 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
       float x = sum[kb][r];
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
-      const int s = s0 + 32 * kb + 8 * (r >> 2) + 4 * lh + (r & 3);
-      if (lr == 0 && s < c.C) {
-        const int64_t at = (int64_t)bg * c.C + s;
+      const int at = (wave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+      // (the list's end repeats no slot: a last, short block leaves its surplus out)
+      if (lr == 0 && at < min(KW, c.C - kbk * KW)) {
+        const int64_t s = lslot[at], slot = (int64_t)bg * c.C + s;
         if (pl.weight_parts > 1) ((float*)a.ws)[pl.weights + ((int64_t)bg * pl.weight_parts + part) * c.C + s] = x;
-        else a.weight_out[at] = kp[kb][r] < 0 ? 0.f : fmaf(a.decay, c.weight[at], x);
+        else a.weight_out[slot] = lpos[at] >= 0x80000000u ? 0.f : fmaf(a.decay, c.weight[slot], x);
       }
     }
 }
@@ -856,7 +1048,8 @@ __global__ __launch_bounds__(256) void weights_join_kernel(TokenCacheArgs c, Tok
 }
 
 template <typename T, int D>
-hipError_t attend_launch(const TokenCacheArgs& c, const TokenAttend& a, int kind, hipStream_t s) {
+hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, int kind, hipStream_t s) {
+  a.rep_inv = (uint32_t)((((uint64_t)1 << 32) + a.rep - 1) / a.rep);
   const int64_t R = (int64_t)a.n * a.rep;
   const int BG = c.B * c.G;
   if (a.n == 0) {  // no rows: the weights only fade
@@ -869,21 +1062,22 @@ hipError_t attend_launch(const TokenCacheArgs& c, const TokenAttend& a, int kind
     return hipGetLastError();
   }
   const TokenAttendPlan pl = token_attend_plan(c, a.n, a.rep, kind, a.weight_out != nullptr);
-  const int slot_blocks = (c.C + 255) / 256;
   const int64_t row_blocks = ((int64_t)BG * R * (D / 4) + 255) / 256;
+  const bool wide = (int64_t)BG * c.C >= 1 << 19;
+  const int slot_blocks = (c.C + (wide ? 1023 : 255)) / (wide ? 1024 : 256);
+  auto finish = [&](bool slots) {
+    const dim3 grid((unsigned)(row_blocks + (slots ? (int64_t)BG * slot_blocks : 0)));
+    if (wide) hipLaunchKernelGGL((finish_kernel<T, D, 4>), grid, dim3(256), 0, s, c, a, pl, (int)row_blocks, slot_blocks);
+    else hipLaunchKernelGGL((finish_kernel<T, D, 1>), grid, dim3(256), 0, s, c, a, pl, (int)row_blocks, slot_blocks);
+  };
   if (pl.by_keys) {
     hipLaunchKernelGGL((attend_keys_kernel<T, D>), dim3(pl.splits, pl.row_tiles, BG), dim3(256), 0, s, c, a, pl);
-    if (pl.splits > 1 || a.weight_out)
-      hipLaunchKernelGGL((finish_kernel<T, D>),
-                         dim3((unsigned)(row_blocks + (a.weight_out ? (int64_t)BG * slot_blocks : 0))), dim3(256), 0, s, c,
-                         a, pl, (int)row_blocks, slot_blocks);
+    if (pl.splits > 1 || a.weight_out) finish(a.weight_out != nullptr);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((attend_rows_kernel<T, D>), dim3((unsigned)(pl.row_tiles * pl.splits * BG)), dim3(256), 0, s, c, a,
                      pl);
-  if (pl.splits > 1)
-    hipLaunchKernelGGL((finish_kernel<T, D>), dim3((unsigned)row_blocks), dim3(256), 0, s, c, a, pl, (int)row_blocks,
-                       slot_blocks);
+  if (pl.splits > 1) finish(false);
   if (a.weight_out) {
     constexpr int KW = sizeof(T) == 2 ? 256 : 128;
     hipLaunchKernelGGL((weights_kernel<T, D>), dim3((unsigned)((c.C + KW - 1) / KW * pl.weight_parts), (unsigned)BG),
@@ -913,13 +1107,17 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   p.row_tiles = (int)up(R, p.by_keys ? 32 : 128);
   const int64_t wgs = BG * p.row_tiles;
   if (p.by_keys) {
-    // three workgroups a CU, but at least two tiles of 32 slots a wave
-    p.splits = (int)clamp(up(768, wgs), 1, clamp(up(c.C, 256), 1, 128));
+    // four rounds of two workgroups a CU (requests of unlike length keep all CUs busy), but
+    // at least two tiles of 32 slots a wave
+    p.splits = (int)clamp(up(2048, wgs), 1, clamp(up(c.C, 256), 1, 128));
   } else {
-    // enough workgroups for two a CU, parts of at least 512 slots
-    p.splits = wgs >= 384 ? 1 : (int)clamp(512 / wgs, 1, clamp(c.C / 512, 1, 16));
+    // slots whose byte offsets from the first fit 32 bits
+    const int64_t step = (kind == 2 ? 4 : 2) * (c.ks[2] > c.vs[2] ? c.ks[2] : c.vs[2]);
+    p.scan = (int)clamp(((int64_t)1 << 32) / (step > 0 ? step : 1) / 64 * 64 - 64, 64, kScan);
+    // two workgroups a CU, in parts of at least two tiles
+    p.splits = (int)clamp(up(512, wgs), 1, clamp(c.C / 128, 1, 16));
     const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
-    p.weight_parts = kw >= 384 ? 1 : (int)clamp(512 / kw, 1, clamp(R / 256, 1, 64));
+    p.weight_parts = (int)clamp(512 / kw, 1, clamp(R / 256, 1, 64));
   }
   int64_t at = 0;
   auto take = [&](int64_t floats) {
@@ -931,7 +1129,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     p.part_o = take(BG * p.splits * R * c.D);
     p.part_ml = take(BG * p.splits * R * 2);
   }
-  if (weights && p.by_keys) p.scores = take(BG * R * c.C);
+  if (weights && p.by_keys) p.scores = take(BG * R * up(c.C, 32) * 32);
   if (weights && !p.by_keys) {
     p.lse2 = take(BG * R);
     if (p.weight_parts > 1) p.weights = take(BG * p.weight_parts * c.C);

@@ -503,14 +503,16 @@ _ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 
 
 def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> None:
-    """ValueError unless t is a CUDA tensor of this dtype, shape and device, contiguous
+    """ValueError unless t is a GPU tensor of this dtype, shape and device, contiguous
     (strided: along its last dimension only)."""
+    if (t.dtype is dtype and t.shape == shape and (t.device == device if device is not None else t.is_cuda)
+            and t.is_cuda and (t.is_contiguous() or (strided and (t.shape[-1] <= 1 or t.stride(-1) == 1)))):
+        return
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if not t.is_cuda or (device is not None and t.device != device):
         raise ValueError(f"{name} must be on {device or 'a GPU'}, got {t.device}")
-    if not (t.is_contiguous() or (strided and (t.shape[-1] <= 1 or t.stride(-1) == 1))):
-        raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
+    raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
 
 
 def _dtype_code(t, name: str) -> int:
@@ -524,23 +526,25 @@ def _dtype_code(t, name: str) -> int:
 def _call_on(device, stream, fn, *args) -> None:
     """fn(*args, stream) with `device` current; stream defaults to its current one."""
     import torch
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
+    index = device.index
+    if stream is None:  # (the handle alone: a Stream object costs 1.5 us, a launch 3)
+        handle = torch._C._cuda_getCurrentRawStream(index)
     elif stream.device != device:
         raise ValueError(f"stream of {stream.device} for tensors on {device}")
-    if torch.cuda.current_device() == device.index:
-        st = fn(*args, stream.cuda_stream)
+    else:
+        handle = stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        st = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            st = fn(*args, stream.cuda_stream)
+            st = fn(*args, handle)
     if st != FD_OK:
         _check(st)
 
 
-def _new(shape, dtype, device, stream):
-    """An uninitialised tensor that work on `stream` may use until it is done."""
-    import torch
-    t = torch.empty(shape, dtype=dtype, device=device)
+def _new(like, shape, dtype, stream):
+    """An uninitialised tensor on like's GPU that work on `stream` may use until it is done."""
+    t = like.new_empty(shape, dtype=dtype)
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -596,7 +600,7 @@ class Rope:
         _need(coords, "coords", torch.int32, (tokens, self.n_axes) if coords.dim() == 2 or self.n_axes > 1 else (tokens,),
               dev)
         if out is None:
-            out = _new(x.shape, x.dtype, dev, stream)
+            out = _new(x, x.shape, x.dtype, stream)
         else:
             _need(out, "out", x.dtype, x.shape, dev, strided=True)
         _call_on(dev, stream, load_library().fd_rope_device, self._p, x.data_ptr(), dt, tokens, heads, dim,
@@ -658,7 +662,7 @@ class TokenCache:
     def choose(self, pos, keep_first: int = 0, keep_recent: int = 0, stream=None):
         """Slots [batch, groups, n] for new tokens at pos [batch, n] (fd_token_slots_device)."""
         import torch
-        slots = _new((self.batch, self.groups, pos.shape[-1]), torch.int32, self.pos.device, stream)
+        slots = _new(self.pos, (self.batch, self.groups, pos.shape[-1]), torch.int32, stream)
         fd_token_slots_device(self.pos, self.weight, pos, slots, keep_first, keep_recent, stream)
         return slots
 
@@ -704,10 +708,10 @@ class TokenCache:
         elif track:
             weight_out = self.weight
         if out is None:
-            out = _new(q.shape, q.dtype, dev, stream)
+            out = _new(q, q.shape, q.dtype, stream)
         else:
             _need(out, "out", q.dtype, q.shape, dev, strided=True)
-        lse = _new((B, heads, n), torch.float32, dev, stream)
+        lse = _new(self.weight, (B, heads, n), torch.float32, stream)
         lib, I3 = load_library(), ctypes.c_int64 * 3
         key = (heads, n, weight_out is not None)
         size = self._ws.get(key)
@@ -715,7 +719,7 @@ class TokenCache:
             b = ctypes.c_size_t()
             _check(lib.fd_token_attend_workspace(self._p, heads, n, int(key[2]), ctypes.byref(b)))
             size = self._ws[key] = b.value
-        ws = _new((size,), torch.uint8, dev, stream)
+        ws = _new(q, (size,), torch.uint8, stream)
         _call_on(dev, stream, lib.fd_token_attend_device, self._p, q.data_ptr(), I3(*q.stride()[:3]), heads, n,
                  pos.data_ptr(), D ** -0.5 if scale is None else scale, int(causal), out.data_ptr(),
                  I3(*out.stride()[:3]), lse.data_ptr(), decay,

@@ -121,7 +121,8 @@ BAD_CACHES = [(dict(struct_size=1), INVALID), (dict(dtype=3), INVALID), (dict(ba
               (dict(pos=None), INVALID), (dict(weight=None), INVALID), (dict(k=A + 8), INVALID),
               (dict(v=A + 2), INVALID), (dict(pos=A + 1), INVALID), (dict(k_stride=(2048, 1024, 63)), INVALID),
               (dict(k_stride=(2048, 1024, 68)), INVALID), (dict(v_stride=(0, 1024, 64)), INVALID),
-              (dict(v_stride=(2048, -1024, 64)), INVALID), (dict(v_stride=(1 << 48, 1024, 64)), INVALID)]
+              (dict(v_stride=(2048, -1024, 64)), INVALID), (dict(v_stride=(1 << 48, 1024, 64)), INVALID),
+              (dict(v_stride=(1 << 40, 1 << 30, 1 << 23)), UNSUPPORTED)]
 
 
 def _append_call(lib, cache=None, rope=None, k=A, ks=(512, 128, 64), v=A, vs=(512, 128, 64), n=4, pos=A, coords=None,
@@ -172,7 +173,7 @@ def test_attend_refusals():
                dict(decay=math.inf), dict(decay=math.nan), dict(qs=(1024, 256, 60)), dict(qs=(1024, 0, 64)),
                dict(os_=(1024, 250, 64)), dict(ws=None), dict(ws=A + 8), dict(size=need - 1), dict(size=0)):
         assert _attend_call(lib, **kw) == INVALID, kw
-    for kw in (dict(heads=4, n=1 << 24), dict(heads=2 << 20, n=64)):
+    for kw in (dict(heads=4, n=1 << 24), dict(heads=514, n=1)):
         assert _attend_call(lib, **kw) == UNSUPPORTED, kw
     huge = cache_struct(batch=300, groups=200, capacity=1 << 20, k_stride=(1 << 40, 1 << 30, 64),
                         v_stride=(1 << 40, 1 << 30, 64))
