@@ -505,10 +505,15 @@ typedef struct fd_token_cache {
  * tokens in order: empty slots are filled first, then the least attended tokens are
  * replaced, recent and first ones only when no other is left. NaN weights order as
  * -infinity, -0 as 0. slot_pos, weight [batch][groups][capacity] are read only; slots
- * [batch][groups][n]. n <= capacity and n <= 65536, keep_first, keep_recent >= 0. */
+ * [batch][groups][n]. n <= capacity and n <= 65536, keep_first, keep_recent >= 0.
+ * workspace: 4-byte aligned, at least fd_token_slots_workspace bytes (0 up to 16384
+ * slots: may be NULL); its contents mean nothing between calls, calls that may overlap
+ * need one each. */
+fd_status fd_token_slots_workspace(int32_t batch, int32_t groups, int32_t capacity, int32_t n, size_t* bytes);
 fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, int32_t batch, int32_t groups,
                                 int32_t capacity, const int32_t* pos, int32_t n, int32_t keep_first,
-                                int32_t keep_recent, int32_t* slots, void* stream);
+                                int32_t keep_recent, int32_t* slots, void* workspace, size_t workspace_bytes,
+                                void* stream);
 
 /* Write n new tokens per request into their slots: k (rotated by `rope` at
  * coords[batch][n][n_axes], computed in fp32 and rounded once; NULL rope: as it is) and v,

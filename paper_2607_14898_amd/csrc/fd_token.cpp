@@ -159,20 +159,40 @@ fd_status fd_rope_device(const fd_rope* rope, const void* x, int32_t dtype, int6
   return launched(fd::rope_rows(r, w, kind, (hipStream_t)stream), "rotary");
 }
 
-fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, int32_t batch, int32_t groups,
-                                int32_t capacity, const int32_t* pos, int32_t n, int32_t keep_first,
-                                int32_t keep_recent, int32_t* slots, void* stream) {
+// Sizes of a choice of slots.
+static fd_status check_slots(int32_t batch, int32_t groups, int32_t capacity, int32_t n) {
   if (batch < 1 || groups < 1 || capacity < 1 || n < 0)
     return fail(FD_ERR_INVALID_ARGUMENT, "batch, groups and capacity must be positive, n >= 0");
   if (capacity > FD_TOKEN_MAX_CAPACITY || (int64_t)batch * groups > 65535)
     return fail(FD_ERR_UNSUPPORTED, "capacity above 2^24, or more than 65535 (request, group) pairs");
   if (n > capacity || n > fd::kMaxSlotTokens)
     return fail(FD_ERR_INVALID_ARGUMENT, "%d new tokens exceed the capacity %d or 65536", n, capacity);
+  return FD_OK;
+}
+
+fd_status fd_token_slots_workspace(int32_t batch, int32_t groups, int32_t capacity, int32_t n, size_t* bytes) {
+  const fd_status st = check_slots(batch, groups, capacity, n);
+  if (st != FD_OK) return st;
+  if (!bytes) return fail(FD_ERR_INVALID_ARGUMENT, "NULL pointer");
+  *bytes = (size_t)fd::token_slots_workspace(batch, groups, capacity, n);
+  return FD_OK;
+}
+
+fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, int32_t batch, int32_t groups,
+                                int32_t capacity, const int32_t* pos, int32_t n, int32_t keep_first,
+                                int32_t keep_recent, int32_t* slots, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  const fd_status st = check_slots(batch, groups, capacity, n);
+  if (st != FD_OK) return st;
   if (keep_first < 0 || keep_recent < 0) return fail(FD_ERR_INVALID_ARGUMENT, "keep_first and keep_recent must be >= 0");
   if (n == 0) return FD_OK;
   if (!slot_pos || !weight || !pos || !slots) return fail(FD_ERR_INVALID_ARGUMENT, "NULL pointer");
   if (((uintptr_t)slot_pos | (uintptr_t)weight | (uintptr_t)pos | (uintptr_t)slots) % 4)
     return fail(FD_ERR_INVALID_ARGUMENT, "misaligned pointer");
+  const int64_t need = fd::token_slots_workspace(batch, groups, capacity, n);
+  if (need > 0 && (!workspace || (uintptr_t)workspace % 4 || workspace_bytes < (size_t)need))
+    return fail(FD_ERR_INVALID_ARGUMENT, "workspace of %zu bytes, %lld needed (4-byte aligned)", workspace_bytes,
+                (long long)need);
   fd::TokenSlots a;
   a.slot_pos = slot_pos;
   a.weight = weight;
@@ -184,6 +204,7 @@ fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, in
   a.n = n;
   a.keep_first = keep_first;
   a.keep_recent = keep_recent;
+  a.ws = workspace;
   return launched(fd::token_slots(a, (hipStream_t)stream), "slot choice");
 }
 

@@ -59,9 +59,14 @@ struct TokenSlots {
   int* slots = nullptr;            // [B][G][n]
   int B = 1, G = 1, C = 1, n = 1;
   int keep_first = 0, keep_recent = 0;
+  void* ws = nullptr;              // token_slots_workspace bytes
+  // of the two launches of a large choice (set by the launcher)
+  int chunks = 0;                  // chunks of slots
+  const int* list_in = nullptr;    // [B G][chunks][n] what they chose (second launch)
 };
 constexpr int kMaxSlotTokens = 65536;  // new tokens of one choice
-hipError_t token_slots(const TokenSlots& a, hipStream_t stream);
+int64_t token_slots_workspace(int batch, int groups, int capacity, int n);
+hipError_t token_slots(TokenSlots a, hipStream_t stream);
 
 // Attention over a token cache. Row r = i rep + h of a (request, group) is query
 // token i of the group's head h (R = n rep rows), so that a tile of rows covers

@@ -117,7 +117,8 @@ def load_library() -> ctypes.CDLL:
         "fd_rope_frequencies": (I32, [I32, ctypes.c_double, I32] + [ctypes.c_double] * 4 +
                                 [P, ctypes.POINTER(ctypes.c_float)]),
         "fd_rope_device": (I32, [P, P, I32, I64, I32, I32, I64, I64, P, P, I64, I64, P]),
-        "fd_token_slots_device": (I32, [P, P, I32, I32, I32, P, I32, I32, I32, P, P]),
+        "fd_token_slots_workspace": (I32, [I32, I32, I32, I32, ctypes.POINTER(SZ)]),
+        "fd_token_slots_device": (I32, [P, P, I32, I32, I32, P, I32, I32, I32, P, P, SZ, P]),
         "fd_token_append_device": (I32, [P, P, P, P, P, P, I32, P, P, P, P]),
         "fd_token_attend_workspace": (I32, [P, I32, I32, I32, ctypes.POINTER(SZ)]),
         "fd_token_attend_device": (I32, [P, P, P, I32, I32, P, ctypes.c_float, I32, P, P, P, ctypes.c_float, P, P, SZ, P]),
@@ -619,8 +620,14 @@ def fd_token_slots_device(slot_pos, weight, pos, slots, keep_first: int = 0, kee
     _need(weight, "weight", torch.float32, slot_pos.shape, dev)
     _need(pos, "pos", torch.int32, (B, n), dev)
     _need(slots, "slots", torch.int32, (B, G, n), dev)
-    _call_on(dev, stream, load_library().fd_token_slots_device, slot_pos.data_ptr(), weight.data_ptr(), B, G, C,
-             pos.data_ptr(), n, keep_first, keep_recent, slots.data_ptr())
+    lib, size, ws = load_library(), 0, None
+    if C > 16384:  # (smaller choices need no workspace)
+        b = ctypes.c_size_t()
+        _check(lib.fd_token_slots_workspace(B, G, C, n, ctypes.byref(b)))
+        size = b.value
+        ws = _new(slots, (size,), torch.uint8, stream)
+    _call_on(dev, stream, lib.fd_token_slots_device, slot_pos.data_ptr(), weight.data_ptr(), B, G, C, pos.data_ptr(), n,
+             keep_first, keep_recent, slots.data_ptr(), None if ws is None else ws.data_ptr(), size)
 
 
 class TokenCache:

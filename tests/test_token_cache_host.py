@@ -90,8 +90,8 @@ def test_rope_refusals():
     assert _rope_call(lib, tokens=0, x=None, out=None, coords=None) == fdb.FD_OK
 
 
-def _slots_call(lib, at=A, w=A, B=2, G=2, C=16, pos=A, n=4, first=0, recent=0, out=A):
-    return lib.fd_token_slots_device(at, w, B, G, C, pos, n, first, recent, out, None)
+def _slots_call(lib, at=A, w=A, B=2, G=2, C=16, pos=A, n=4, first=0, recent=0, out=A, ws=None, size=0):
+    return lib.fd_token_slots_device(at, w, B, G, C, pos, n, first, recent, out, ws, size, None)
 
 
 def test_slots_refusals():
@@ -103,6 +103,15 @@ def test_slots_refusals():
     for kw in (dict(C=(1 << 24) + 1), dict(B=256, G=256)):
         assert _slots_call(lib, **kw) == UNSUPPORTED, kw
     assert _slots_call(lib, n=0, at=None) == fdb.FD_OK
+    size = ctypes.c_size_t()
+    for args, need in (((2, 2, 16384, 99), 0), ((2, 2, 16385, 1), 0), ((2, 2, 40000, 100), 4 * 3 * 100 * 4),
+                       ((1, 1, 40000, 30000), 0)):
+        assert lib.fd_token_slots_workspace(*args, ctypes.byref(size)) == fdb.FD_OK and size.value == need, args
+    assert lib.fd_token_slots_workspace(2, 2, 40000, 100, None) == INVALID
+    assert lib.fd_token_slots_workspace(2, 2, 100, 101, ctypes.byref(size)) == INVALID
+    assert lib.fd_token_slots_workspace(2, 2, (1 << 24) + 1, 1, ctypes.byref(size)) == UNSUPPORTED
+    for kw in (dict(ws=None), dict(ws=A, size=4799), dict(ws=A + 2, size=4800)):
+        assert _slots_call(lib, C=40000, n=100, **kw) == INVALID, kw
 
 
 def cache_struct(**kw):
