@@ -23,6 +23,8 @@
 // added (slow, and never taken by finite data).
 #include "fd_token.h"
 
+#include <stdint.h>
+
 #include <type_traits>
 
 namespace fd {
@@ -133,6 +135,20 @@ __device__ __forceinline__ float other_half_max(float x) {
 __device__ __forceinline__ float other_half_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Sum over the 32 lanes of a half, in its last lane.
+__device__ __forceinline__ float half_sum(float x) {
+  auto moved = [](float y, auto ctrl, auto rows) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(y), decltype(ctrl)::value, decltype(rows)::value,
+                                                      0xf, false));
+  };
+  using std::integral_constant;
+  x += moved(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // 1, 2, 4, 8 lanes up in 16
+  x += moved(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  x += moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // rows 0, 2 into 1, 3
+  return x;
 }
 __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
   for (int o = 32; o > 0; o >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, o));
@@ -863,7 +879,7 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
 // workgroup's slots are taken in the order seen by every row, by some rows, empty, so
 // that a mask costs the waves with the call's own tokens alone.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
   constexpr int KB = sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
   constexpr int KW = 128 * KB;                // slots of a workgroup
@@ -979,7 +995,7 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
   for (int64_t t = t0; t < t1; ++t) {
     const int cur = (int)(t - t0) & 1;
     if (t + 1 < t1) load(t + 1);
-#pragma unroll
+#pragma unroll 1
     for (int rb = 0; rb < RT / 32; ++rb) {
       const uint32_t lim = slim[cur][32 * rb + lr];
       if (__ballot(lim > p_min) == 0) continue;
@@ -1024,12 +1040,10 @@ __global__ __launch_bounds__(256, 2) void weights_kernel(TokenCacheArgs c, Token
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      float x = sum[kb][r];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) x += __shfl_xor(x, o);
+      const float x = half_sum(sum[kb][r]);
       const int at = (wave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
       // (the list's end repeats no slot: a last, short block leaves its surplus out)
-      if (lr == 0 && at < min(KW, c.C - kbk * KW)) {
+      if (lr == 31 && at < min(KW, c.C - kbk * KW)) {
         const int64_t s = lslot[at], slot = (int64_t)bg * c.C + s;
         if (pl.weight_parts > 1) ((float*)a.ws)[pl.weights + ((int64_t)bg * pl.weight_parts + part) * c.C + s] = x;
         else a.weight_out[slot] = lpos[at] >= 0x80000000u ? 0.f : fmaf(a.decay, c.weight[slot], x);
@@ -1106,10 +1120,20 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   p.by_keys = R <= 64;
   p.row_tiles = (int)up(R, p.by_keys ? 32 : 128);
   const int64_t wgs = BG * p.row_tiles;
+  // workgroups that the chip holds at once (by registers and LDS)
+  const int64_t held = 256 * (c.D < 128 ? 3 : kind == 2 ? 1 : 2);
   if (p.by_keys) {
-    // four rounds of two workgroups a CU (requests of unlike length keep all CUs busy), but
-    // at least two tiles of 32 slots a wave
-    p.splits = (int)clamp(up(2048, wgs), 1, clamp(up(c.C, 256), 1, 128));
+    // whole rounds of what is held, of parts that are long beside what a part costs by
+    // itself (about 96 slots' time) but leave two tiles of 32 slots a wave
+    int64_t best = INT64_MAX;
+    const int64_t most = clamp(up(c.C, 256), 1, 256);
+    for (int64_t s = 1; s <= most; ++s) {
+      const int64_t cost = up(wgs * s, held) * (up(c.C, s) + 96);
+      if (cost < best) {
+        best = cost;
+        p.splits = (int)s;
+      }
+    }
   } else {
     // slots whose byte offsets from the first fit 32 bits
     const int64_t step = (kind == 2 ? 4 : 2) * (c.ks[2] > c.vs[2] ? c.ks[2] : c.vs[2]);
@@ -1117,7 +1141,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     // two workgroups a CU, in parts of at least two tiles
     p.splits = (int)clamp(up(512, wgs), 1, clamp(c.C / 128, 1, 16));
     const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
-    p.weight_parts = (int)clamp(512 / kw, 1, clamp(R / 256, 1, 64));
+    p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
   }
   int64_t at = 0;
   auto take = [&](int64_t floats) {
