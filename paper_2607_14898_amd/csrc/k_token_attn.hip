@@ -743,7 +743,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
 // rows (D / 4 threads each), the others add up what rows gave kFinishSlots slots each,
 // from the scores that attend_keys_kernel kept (4 bytes a row and slot, beside 4 D of a
 // 16-bit key and value). Each of those works out its rows' log-sums from the parts by
-// itself, 16 threads a row. Parts are read side by side throughout: a chain of dependent
+// itself, 16 threads a row (64 for many parts). Parts are read side by side throughout: a chain of dependent
 // loads per part cost 0.7 us each.
 // Four slots a thread once that still leaves two workgroups a CU.
 constexpr int kFinishRows = 64;
@@ -762,11 +762,17 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
     const float2* ml = reinterpret_cast<const float2*>(ws + pl.part_ml) + bg * S * R + r;
     M = -INFINITY;
     L = 0.f;
-    for (int s = j; s < S; s += W) {
-      const float2 x = ml[(int64_t)s * R];
-      const float m = fmaxf(M, x.x);
-      if (m != -INFINITY) L = L * __builtin_amdgcn_exp2f(M - m) + x.y * __builtin_amdgcn_exp2f(x.x - m);
-      M = m;
+    for (int s = j; s < S; s += 4 * W) {
+      float2 x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = ml[(int64_t)min(s + e * W, S - 1) * R];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (s + e * W >= S) break;
+        const float m = fmaxf(M, x[e].x);
+        if (m != -INFINITY) L = L * __builtin_amdgcn_exp2f(M - m) + x[e].y * __builtin_amdgcn_exp2f(x[e].x - m);
+        M = m;
+      }
     }
 #pragma unroll
     for (int o = 1; o < W; o <<= 1) {
@@ -780,9 +786,12 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
     }
   };
   if ((int)blockIdx.x < row_blocks) {
+    // (many parts are shared by pl.join groups of a row's threads, which meet in LDS)
     constexpr int TPR = D / 4, RPB = 256 / TPR;
+    __shared__ float4 s_o[256];
     const int64_t rows = (int64_t)c.B * c.G * R;
-    const int64_t x_ = (int64_t)blockIdx.x * RPB + tid / TPR, x = min(x_, rows - 1);  // row over all (b, g)
+    const int group = tid / TPR % pl.join;
+    const int64_t x_ = (int64_t)blockIdx.x * (RPB / pl.join) + tid / TPR / pl.join, x = min(x_, rows - 1);
     const int j = tid % TPR, d = 4 * j;
     const int64_t bg = x / R;
     const int r = (int)(x - bg * R);
@@ -793,19 +802,36 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* po = ws + pl.part_o + (bg * S * R + r) * D + d;
     const float2* ml = reinterpret_cast<const float2*>(ws + pl.part_ml) + bg * S * R + r;
-#pragma unroll 4
-    for (int s = 0; s < S; ++s) {
-      const float ms = ml[(int64_t)s * R].x;
-      const float4 p = *reinterpret_cast<const float4*>(po + (int64_t)s * R * D);
-      const float f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
-      if (f != 0.f) {  // (a part that saw nothing holds no number)
-        o.x = fmaf(f, p.x, o.x);
-        o.y = fmaf(f, p.y, o.y);
-        o.z = fmaf(f, p.z, o.z);
-        o.w = fmaf(f, p.w, o.w);
+    for (int s0 = group; s0 < S; s0 += 4 * pl.join) {
+      float ms[4];
+      float4 p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t s = min(s0 + e * pl.join, S - 1);
+        ms[e] = s0 + e * pl.join < S ? ml[s * R].x : -INFINITY;
+        p[e] = *reinterpret_cast<const float4*>(po + s * R * D);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float f = ms[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[e] - M);
+        if (f != 0.f) {  // (a part that saw nothing holds no number)
+          o.x = fmaf(f, p[e].x, o.x);
+          o.y = fmaf(f, p[e].y, o.y);
+          o.z = fmaf(f, p[e].z, o.z);
+          o.w = fmaf(f, p[e].w, o.w);
+        }
       }
     }
-    if (x_ >= rows) return;
+    if (pl.join > 1) {
+      s_o[tid] = o;
+      __syncthreads();
+      if (group == 0)
+        for (int y = 1; y < pl.join; ++y) {
+          const float4 p = s_o[tid + y * TPR];
+          o = make_float4(o.x + p.x, o.y + p.y, o.z + p.z, o.w + p.w);
+        }
+    }
+    if (x_ >= rows || group != 0) return;
     const Row w = row_of(a, b, g, r, R);
     if (M == -INFINITY) o = make_float4(0.f, 0.f, 0.f, 0.f);
     else o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
@@ -833,14 +859,19 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
   for (int r0 = 0; r0 < R; r0 += kFinishRows) {
     const int m = min(kFinishRows, R - r0);
     __syncthreads();
-    for (int q = tid / 16; q < (m + 15) / 16 * 16; q += 16) {
-      float M, L;
-      total(bg, r0 + min(q, m - 1), tid % 16, std::integral_constant<int, 16>{}, M, L);
-      if (tid % 16 == 0 && q < m) {
-        s_l2[q] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
-        s_lim[q] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + q, R).lim;
+    auto sums = [&](auto width) {
+      constexpr int W = decltype(width)::value, RG = 256 / W;
+      for (int q = tid / W; q < (m + RG - 1) / RG * RG; q += RG) {
+        float M, L;
+        total(bg, r0 + min(q, m - 1), tid % W, width, M, L);
+        if (tid % W == 0 && q < m) {
+          s_l2[q] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
+          s_lim[q] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + q, R).lim;
+        }
       }
-    }
+    };
+    if (S > 64) sums(std::integral_constant<int, 64>{});
+    else sums(std::integral_constant<int, 16>{});
     __syncthreads();
     const float* sc[NS];
 #pragma unroll
@@ -1076,7 +1107,8 @@ hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, int kind, hipSt
     return hipGetLastError();
   }
   const TokenAttendPlan pl = token_attend_plan(c, a.n, a.rep, kind, a.weight_out != nullptr);
-  const int64_t row_blocks = ((int64_t)BG * R * (D / 4) + 255) / 256;
+  const int rows_each = 256 / (D / 4) / pl.join;
+  const int64_t row_blocks = ((int64_t)BG * R + rows_each - 1) / rows_each;
   const bool wide = (int64_t)BG * c.C >= 1 << 19;
   const int slot_blocks = (c.C + (wide ? 1023 : 255)) / (wide ? 1024 : 256);
   auto finish = [&](bool slots) {
@@ -1138,8 +1170,23 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     // slots whose byte offsets from the first fit 32 bits
     const int64_t step = (kind == 2 ? 4 : 2) * (c.ks[2] > c.vs[2] ? c.ks[2] : c.vs[2]);
     p.scan = (int)clamp(((int64_t)1 << 32) / (step > 0 ? step : 1) / 64 * 64 - 64, 64, kScan);
-    // two workgroups a CU, in parts of at least two tiles
-    p.splits = (int)clamp(up(512, wgs), 1, clamp(c.C / 128, 1, 16));
+    // Parts by a model of what was measured, in us: a tile of 64 slots takes a workgroup
+    // alone on its CU t, L of them on one CU 0.65 L t, a workgroup's ends six tiles' time, and
+    // joining parts a launch and its traffic. (1560 tokens x 8 heads, 3 groups, 4680 slots, 64
+    // dims: one part 118 us, two 87 + 9, three 88 + 12. 61 tokens x 4, 6 groups, 1531 slots,
+    // fp32: two parts 64 us, eleven 21.) More parts only where they gain 5%.
+    const double t = kind == 2 ? 0.065 * c.D : c.D == 128 ? 1.75 : c.D == 64 ? 1.2 : 0.9;
+    double best = 0.0;
+    const int64_t most = clamp(c.C / 128, 1, 64);
+    for (int64_t s = 1; s <= most; ++s) {
+      const double load = 0.65 * (double)up(wgs * s, 256);
+      const double cost = ((double)c.C / (64.0 * s) + 6.0) * t * (load < 1.0 ? 1.0 : load) +
+                          (s > 1 ? 4.0 + (double)(s * BG * R * c.D) * 8.0 / 5e6 : 0.0);
+      if (s == 1 || cost < 0.95 * best) {
+        best = cost;
+        p.splits = (int)s;
+      }
+    }
     const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
     p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
   }
@@ -1149,6 +1196,8 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     at += up(floats, 64) * 64;
     return o;
   };
+  const int groups = 256 / (c.D / 4);  // of a row's threads in a workgroup of finish_kernel
+  p.join = p.splits >= 32 ? groups : p.splits >= 8 ? 4 : 1;
   if (p.splits > 1 || (p.by_keys && weights)) {
     p.part_o = take(BG * p.splits * R * c.D);
     p.part_ml = take(BG * p.splits * R * 2);
