@@ -332,7 +332,9 @@ __global__ __launch_bounds__(kThreads) void slots_kernel(TokenSlots a) {
   }
 }
 
-// One new token: the least (class, weight, slot).
+// One new token: the least (class, weight, slot). U loads of each array are under way (a
+// few thousand slots are one or two a thread: eight would load the last one over and over).
+template <int U>
 __global__ __launch_bounds__(kThreads) void slot_least_kernel(TokenSlots a) {
   __shared__ uint64_t part[kWaves];
   const int tid = threadIdx.x;
@@ -340,10 +342,21 @@ __global__ __launch_bounds__(kThreads) void slot_least_kernel(TokenSlots a) {
   const int p = a.pos[blockIdx.x / a.G];
   const int recent_from = max(p, 0) - a.keep_recent;
   uint64_t best = ~0ull;
-  for (int s = tid; s < a.C; s += kThreads) {
-    const int c = slot_class(a.slot_pos[base + s], recent_from, a.keep_first);
-    const uint64_t k = (((uint64_t)c << 32 | (c ? weight_key(a.weight[base + s]) : 0)) << 24) | (uint32_t)s;
-    best = k < best ? k : best;
+  for (int s0 = tid; s0 < a.C; s0 += U * kThreads) {
+    int q[U];
+    float w[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x) {
+      const int64_t at = base + min(s0 + x * kThreads, a.C - 1);
+      q[x] = a.slot_pos[at];
+      w[x] = a.weight[at];
+    }
+#pragma unroll
+    for (int x = 0; x < U; ++x) {  // (the last slot may come twice: the least is the same)
+      const int c = slot_class(q[x], recent_from, a.keep_first);
+      const uint64_t k = (((uint64_t)c << 32 | (c ? weight_key(w[x]) : 0)) << 24) | (uint32_t)min(s0 + x * kThreads, a.C - 1);
+      best = k < best ? k : best;
+    }
   }
   for (int o = 32; o > 0; o >>= 1) {
     const uint64_t y = __shfl_xor((unsigned long long)best, o);
@@ -392,7 +405,8 @@ hipError_t token_slots(TokenSlots a, hipStream_t s) {
     return choose(a, (unsigned)(a.B * a.G), (int)chunks * a.n, s);
   }
   if (a.n > 1) return choose(a, (unsigned)(a.B * a.G), a.C, s);
-  hipLaunchKernelGGL(slot_least_kernel, grid, dim3(kThreads), 0, s, a);
+  if (a.C <= 2 * kThreads) hipLaunchKernelGGL(slot_least_kernel<1>, grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL(slot_least_kernel<8>, grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

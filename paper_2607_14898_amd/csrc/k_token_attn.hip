@@ -19,8 +19,8 @@
 // Whatever empty and hidden slots hold must not matter. Scores are replaced, not added
 // to. V of empty slots is zeroed as it is staged. V of slots hidden from some rows alone
 // may hold infinities or NaN, which 0 x V would spread: rows that end up not finite are
-// computed once more with such elements as zeros, and those of visible slots are then
-// added (slow, and never taken by finite data).
+// computed once more with such elements as zeros, and if there were any, those of visible
+// slots are then added (finite data never comes here).
 #include "fd_token.h"
 
 #include <stdint.h>
@@ -285,15 +285,40 @@ template <typename T, int D, bool EXACT> struct Softmax {
       for (int r = 0; r < 16; ++r) t += 0.f * acc[d][r];  // NaN if any is not finite
     return t == 0.f;
   }
-  // Adds the infinities and NaN of one slot's value.
-  __device__ __forceinline__ void add_unbounded(const T* v, int lh) {
+  // A row whose scores were all NaN has no maximum, but it has seen something.
+  __device__ __forceinline__ void close(float sum) {
+    if (m == -INFINITY && sum != sum) m = 0.f;
+  }
+  // Adds the infinities and NaN among the values of slots s0 .. s1 - 1 that the row sees.
+  // The wave looks through several slots at a load; only those that hold some are added.
+  __device__ __forceinline__ void add_unbounded(const T* v, int64_t step, const int* pos, int s0, int s1, uint32_t lim,
+                                                int lane) {
+    using TL = Tile<T, D>;
+    constexpr int SL = 64 / TL::CPR, U = 8;  // slots of a load, loads under way
+    for (int x0 = s0; x0 < s1; x0 += SL * U) {
+      u32x4 c[U];
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+      for (int u = 0; u < U; ++u)
+        c[u] = *reinterpret_cast<const u32x4*>(v + min(x0 + u * SL + lane / TL::CPR, s1 - 1) * step +
+                                               lane % TL::CPR * TL::EPC);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = (float)v[32 * d + 8 * (r >> 2) + 4 * lh + (r & 3)];
-        if (!isfinite(x)) acc[d][r] += x;
+      for (int u = 0; u < U; ++u) {
+        const u32x4 f = finite_part<T>(c[u]);
+        uint64_t bad = __ballot(f.x != c[u].x || f.y != c[u].y || f.z != c[u].z || f.w != c[u].w);
+        while (bad) {
+          const int x = x0 + u * SL + __builtin_ctzll(bad) / TL::CPR;
+          bad &= ~0ull << (__builtin_ctzll(bad) / TL::CPR * TL::CPR + TL::CPR - 1) << 1;
+          if (x >= s1 || (uint32_t)pos[x] >= lim) continue;
+#pragma unroll
+          for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float y = (float)v[x * step + 32 * d + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)];
+              if (!isfinite(y)) acc[d][r] += y;
+            }
+        }
       }
+    }
   }
 };
 
@@ -346,6 +371,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   const int t0 = split * per + wave, t1 = min(tiles, (split + 1) * per);
   u32x4* tile = buf[wave];
   Softmax<T, D, true> sx;
+  bool changed = false;  // some value of this wave's slots is not finite
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
     for (int tc = t0; tc < t1; tc += 4 * 64) {
@@ -360,71 +386,75 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
         if (tc + 8 * (x + 1) >= t1) break;
       }
       while (live) {
-      const int t = tc + 4 * __builtin_ctzll(live);
-      live &= live - 1;
-      const int p = t * 32 + lr < c.C ? ps[t * 32 + lr] : -1;
-      const uint32_t taken = (uint32_t)__ballot(p >= 0);
-      const bool all = (uint32_t)__ballot((uint32_t)p < lim_min) == ~0u;
-      u32x4 kr[NV], vr[NV];
+        const int t = tc + 4 * __builtin_ctzll(live);
+        live &= live - 1;
+        const int p = t * 32 + lr < c.C ? ps[t * 32 + lr] : -1;
+        const uint32_t taken = (uint32_t)__ballot(p >= 0);
+        const bool all = (uint32_t)__ballot((uint32_t)p < lim_min) == ~0u;
+        u32x4 kr[NV], vr[NV];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int idx = j * 64 + lane, kr_ = idx / TL::CPR, ch = idx % TL::CPR;
-        const int64_t s = min(t * 32 + kr_, c.C - 1);
-        kr[j] = *reinterpret_cast<const u32x4*>(kb + s * c.ks[2] + ch * TL::EPC);
-        vr[j] = *reinterpret_cast<const u32x4*>(vb + s * c.vs[2] + ch * TL::EPC);
-      }
-      if (!all) spos[wave][lr] = p;
+        for (int j = 0; j < NV; ++j) {
+          const int idx = j * 64 + lane, kr_ = idx / TL::CPR, ch = idx % TL::CPR;
+          const int64_t s = min(t * 32 + kr_, c.C - 1);
+          kr[j] = *reinterpret_cast<const u32x4*>(kb + s * c.ks[2] + ch * TL::EPC);
+          vr[j] = *reinterpret_cast<const u32x4*>(vb + s * c.vs[2] + ch * TL::EPC);
+        }
+        if (!all) spos[wave][lr] = p;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int idx = j * 64 + lane;
-        tile[TL::k(idx / TL::CPR, idx % TL::CPR)] = kr[j];
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      f32x16 s[1];
+        for (int j = 0; j < NV; ++j) {
+          const int idx = j * 64 + lane;
+          tile[TL::k(idx / TL::CPR, idx % TL::CPR)] = kr[j];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        f32x16 s[1];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) s[0] = Op<T>::mma(TL::k_frag(tile, key_of_row(lr), ks, lh), qf[ks], s[0]);
-      if (a.weight_out && row < R) {  // [tile][row][32]: whole lines, however few the rows
-        float* score = (float*)a.ws + pl.scores + (((int64_t)bg * tiles + t) * R + row) * 32 + 8 * lh;
+        for (int ks = 0; ks < D / 16; ++ks) s[0] = Op<T>::mma(TL::k_frag(tile, key_of_row(lr), ks, lh), qf[ks], s[0]);
+        if (a.weight_out && row < R) {  // [tile][row][32]: whole lines, however few the rows
+          float* score = (float*)a.ws + pl.scores + (((int64_t)bg * tiles + t) * R + row) * 32 + 8 * lh;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          store4(score + 16 * (r >> 3) + (r & 4), s[0][r], s[0][r + 1], s[0][r + 2], s[0][r + 3]);
-      }
-      if (!all) {
+          for (int r = 0; r < 16; r += 4)
+            store4(score + 16 * (r >> 3) + (r & 4), s[0][r], s[0][r + 1], s[0][r + 2], s[0][r + 3]);
+        }
+        if (!all) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if ((uint32_t)spos[wave][16 * (r >> 3) + 8 * lh + (r & 7)] >= w.lim) s[0][r] = -INFINITY;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+          for (int r = 0; r < 16; ++r)
+            if ((uint32_t)spos[wave][16 * (r >> 3) + 8 * lh + (r & 7)] >= w.lim) s[0][r] = -INFINITY;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int idx = j * 64 + lane, vrow = idx / TL::CPR;
-        u32x4 x = vr[j];
-        if (!(taken >> vrow & 1)) x = u32x4{0, 0, 0, 0};
-        if (scrub) x = finite_part<T>(x);
-        tile[TL::v(vrow, idx % TL::CPR)] = x;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      sx.template add<1>(s, cs, tile, 0, lane);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int j = 0; j < NV; ++j) {
+          const int idx = j * 64 + lane, vrow = idx / TL::CPR;
+          u32x4 x = vr[j];
+          if (!(taken >> vrow & 1)) x = u32x4{0, 0, 0, 0};
+          if (scrub) {
+            const u32x4 f = finite_part<T>(x);
+            changed |= f.x != x.x || f.y != x.y || f.z != x.z || f.w != x.w;
+            x = f;
+          }
+          tile[TL::v(vrow, idx % TL::CPR)] = x;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        sx.template add<1>(s, cs, tile, 0, lane);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
     }
-    if (scrub || __ballot(w.lim != 0 && !sx.finite()) == 0) {
-      if (scrub)
+    if (scrub) {
+      if (__ballot(changed))
         for (int t = t0; t < t1; t += 4)
-          for (int x = t * 32; x < min(t * 32 + 32, c.C); ++x)
-            if ((uint32_t)ps[x] < w.lim) sx.add_unbounded(vb + x * c.vs[2], lh);
+          sx.add_unbounded(vb, c.vs[2], ps, t * 32, min(t * 32 + 32, c.C), w.lim, lane);
       break;
     }
+    if (__ballot(w.lim != 0 && !sx.finite()) == 0) break;
   }
 
   if (w.lim == 0) {  // padding: what tiles without a mask gave it does not count
@@ -433,6 +463,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   }
   // the four waves' rows on one shift
   const float lsum = other_half_sum(sx.l);
+  sx.close(lsum);
   if (lh == 0) {
     sm[wave][lr] = sx.m;
     sl[wave][lr] = lsum;
@@ -513,6 +544,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   __shared__ uint16_t list[kScan];
   __shared__ uint32_t slim[2][4];
   __shared__ int scount[2][4];
+  __shared__ int schanged;  // some staged value is not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   // Workgroups are dealt to the 8 XCDs in turn; each XCD takes a contiguous range of
@@ -526,6 +558,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   const int64_t row = (int64_t)rt * 128 + wave * 32 + lr;
   const Row w = row_of(a, b, g, row, R);
   const uint32_t lim_max = lanes_max(w.lim), lim_min = lanes_min(w.lim ? w.lim : ~0u);
+  if (tid == 0) schanged = 0;
   if (lane == 0) {
     slim[0][wave] = lim_max;
     slim[1][wave] = lim_min;
@@ -587,7 +620,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     asm volatile("" ::: "memory");
     if (scrub) {
 #pragma unroll 1
-      for (int idx = tid; idx < KT * TL::CPR; idx += 256) sv[buf][idx] = finite_part<T>(sv[buf][idx]);
+      for (int idx = tid; idx < KT * TL::CPR; idx += 256) {
+        const u32x4 x = sv[buf][idx], f = finite_part<T>(x);
+        if (f.x != x.x || f.y != x.y || f.z != x.z || f.w != x.w) schanged = 1;
+        sv[buf][idx] = f;
+      }
       __syncthreads();
     }
   };
@@ -685,8 +722,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     }
     __syncthreads();
     if (scrub) {
-      for (int x = s_lo; x < s_hi; ++x)
-        if ((uint32_t)ps[x] < w.lim) sx.add_unbounded(vbase + x * c.vs[2], lh);
+      if (schanged) sx.add_unbounded(vbase, c.vs[2], ps, s_lo, s_hi, w.lim, lane);
       break;
     }
     if (!__syncthreads_or(w.lim != 0 && !sx.finite())) break;
@@ -697,6 +733,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     sx.l = 0.f;
   }
   const float L = other_half_sum(sx.l);
+  sx.close(L);
   // (the row's place is worked out again, from a lane the compiler takes for another:
   // kept through the loop it would cost registers that 128 dims do not have)
   int lane_ = lane;

@@ -506,8 +506,8 @@ _ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> None:
     """ValueError unless t is a GPU tensor of this dtype, shape and device, contiguous
     (strided: along its last dimension only)."""
-    if (t.dtype is dtype and t.shape == shape and (t.device == device if device is not None else t.is_cuda)
-            and t.is_cuda and (t.is_contiguous() or (strided and (t.shape[-1] <= 1 or t.stride(-1) == 1)))):
+    if (t.is_cuda and t.dtype is dtype and t.shape == shape and (device is None or t.device == device)
+            and (t.is_contiguous() or (strided and (t.shape[-1] <= 1 or t.stride(-1) == 1)))):
         return
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
@@ -516,9 +516,14 @@ def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> Non
     raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
 
 
+_codes: Dict = {}  # torch dtype -> FD_DTYPE_*
+
+
 def _dtype_code(t, name: str) -> int:
-    import torch
-    code = {torch.float32: FD_DTYPE_F32, torch.bfloat16: FD_DTYPE_BF16, torch.float16: FD_DTYPE_F16}.get(t.dtype)
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: FD_DTYPE_F32, torch.bfloat16: FD_DTYPE_BF16, torch.float16: FD_DTYPE_F16})
+    code = _codes.get(t.dtype)
     if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     return code
@@ -534,7 +539,7 @@ def _call_on(device, stream, fn, *args) -> None:
         raise ValueError(f"stream of {stream.device} for tensors on {device}")
     else:
         handle = stream.cuda_stream
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         st = fn(*args, handle)
     else:
         with torch.cuda.device(device):

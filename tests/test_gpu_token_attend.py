@@ -180,6 +180,41 @@ def test_infinities_and_nan_that_some_rows_do_not_see(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n", [2, 50])
+def test_nan_reaches_the_rows_that_see_it(dtype, n):
+    """A NaN query, and a visible key of NaN, make NaN of exactly the rows and slots that they belong to."""
+    k, v, at, weight, q, pos = make(1, 2, 4, 64, n, 300, dtype, seed=6)
+    at.copy_(torch.arange(300).view(1, 1, -1))
+    pos.copy_(torch.where(torch.arange(n) < n // 2, 150, 299))
+    q[:, 0, 1] = float("nan")         # token 0 (sees 0 .. 150), head 1 of group 0
+    k[0, 1, 200] = float("nan")       # seen by the later tokens of group 1
+    want, tol = ref(k.nan_to_num(0.0), v, at, weight, q.nan_to_num(0.0), pos, 64 ** -0.5, True, 1.0)
+    w = torch.empty_like(weight)
+    out, lse = fdb.TokenCache(k, v, at, weight).attend(q, pos, weight_out=w)
+    bad = torch.zeros(n, 4, dtype=torch.bool)
+    bad[0, 1] = True
+    bad[n // 2:, 2:] = True
+    assert torch.equal(out[0].isnan().all(-1).cpu(), bad) and torch.equal(out[0].isnan().any(-1).cpu(), bad)
+    assert torch.equal(lse[0].isnan().cpu(), bad.T)
+    near(out[0].cpu()[~bad], want[0][0][~bad], tol[0][0][~bad])
+    seen = torch.arange(300) <= 150
+    assert torch.equal(w[0, 0].isnan().cpu(), seen) and bool(w[0, 1].isnan().all())
+    # a slot alone in its part, with a key of NaN
+    at[:, 1] = -1
+    at[0, 1, 290] = 0
+    k[0, 1, 290] = float("nan")
+    out, lse = fdb.TokenCache(k, v, at, weight).attend(q, pos, track=False)
+    assert bool(out[0, :, 2:].isnan().all()) and bool(lse[0, 2:].isnan().all())
+    assert not bool(out[0, n // 2:, :2].isnan().any())
+
+
+@pytest.mark.parametrize("B,G,N,n,C", [(1, 1, 256, 1, 90), (1, 1, 256, 3, 200), (300, 8, 16, 1, 20), (70, 2, 2, 65, 67),
+                                       (1, 1, 2, 1, 9000), (1, 1, 2, 40, 9000)])
+def test_many_heads_requests_and_parts(B, G, N, n, C):
+    check(*make(B, G, N, 32, n, C, BF16, seed=B + C, fill=0.9))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("n", [1, 40])
 def test_scores_far_apart(dtype, n):
     """Logits that rise steeply along the slots, all far below zero, and far above."""
