@@ -64,6 +64,7 @@ template <> struct Op<float> {
   }
 };
 
+constexpr f32x16 kZero = {};
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kRaise = 8.f;  // the running shift rises when a score passes it by 2^8
 
@@ -410,9 +411,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         f32x16 s[1];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[0][r] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) s[0] = Op<T>::mma(TL::k_frag(tile, key_of_row(lr), ks, lh), qf[ks], s[0]);
+        for (int ks = 0; ks < D / 16; ++ks)
+          s[0] = Op<T>::mma(TL::k_frag(tile, key_of_row(lr), ks, lh), qf[ks], ks ? s[0] : kZero);
         if (a.weight_out && row < R) {  // [tile][row][32]: whole lines, however few the rows
           float* score = (float*)a.ws + pl.scores + (((int64_t)bg * tiles + t) * R + row) * 32 + 8 * lh;
 #pragma unroll
@@ -690,10 +690,6 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
         }
         if (any) {
           f32x16 s[KB];
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
           // (a wave at its MFMAs issues them ahead of the other waves on the SIMD, whose
           // exponentials fill in between: 10% at 64 dims, 1% at 128)
           __builtin_amdgcn_s_setprio(3);
@@ -706,7 +702,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[ks][kb], qf[ks], s[kb]);
+            for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[ks][kb], qf[ks], ks ? s[kb] : kZero);
           __builtin_amdgcn_s_setprio(0);
           if (!all) {
 #pragma unroll
@@ -1070,10 +1066,6 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
       const bool all = __ballot(lim > p_max) == ~0ull;
       const float nl = -sl2[cur][32 * rb + lr];
       f32x16 s[KB];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
       // (all fragments are on their way before the first MFMA: left to itself the compiler
       // waits for each of them in turn)
       typename Op<T>::V q[D / 16];
@@ -1083,7 +1075,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[kb][ks], q[ks], s[kb]);
+        for (int kb = 0; kb < KB; ++kb) s[kb] = Op<T>::mma(kf[kb][ks], q[ks], ks ? s[kb] : kZero);
       if (all) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
