@@ -85,6 +85,32 @@ __device__ __forceinline__ void turn_item(const T* x, T* o, int item, int half, 
   }
 }
 
+// A thread's walk over [tokens][rows][items] in steps of 256: divided once, then carried.
+struct Walk {
+  int t, row, item;
+  int dt, drow, ditem, rows, items;
+  __device__ __forceinline__ Walk(int rows_, int items_) : rows(rows_), items(items_) {
+    const int per = rows * items;
+    t = threadIdx.x / per;
+    const int rem = threadIdx.x - t * per;
+    row = rem / items;
+    item = rem - row * items;
+    dt = 256 / per;
+    const int drem = 256 - dt * per;
+    drow = drem / items;
+    ditem = drem - drow * items;
+  }
+  __device__ __forceinline__ void next() {
+    item += ditem;
+    const bool c = item >= items;
+    item -= c ? items : 0;
+    row += drow + c;
+    const bool d = row >= rows;
+    row -= d ? rows : 0;
+    t += dt + d;
+  }
+};
+
 // Workgroup: nt tokens x a range of the heads (gridDim.y ranges).
 template <typename T, bool IL, bool VEC>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs r, RopeRows x, int nt) {
@@ -92,17 +118,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs r, RopeRows x, int n
   const int items = row_items<T, IL, VEC>(x.dim, r.half);
   const int h0 = (int)((int64_t)x.heads * blockIdx.y / gridDim.y);
   const int h1 = (int)((int64_t)x.heads * (blockIdx.y + 1) / gridDim.y);
-  const int per_tok = (h1 - h0) * items;
   for (int64_t t0 = (int64_t)blockIdx.x * nt; t0 < x.tokens; t0 += (int64_t)gridDim.x * nt) {
     const int m = (int)min((int64_t)nt, x.tokens - t0);
     __syncthreads();  // the previous tokens' angles are no longer read
     fill_angles(r, t0, m, cs);
     __syncthreads();
-    for (int i = threadIdx.x; i < m * per_tok; i += 256) {
-      const int t = i / per_tok, rem = i - t * per_tok, h = rem / items, item = rem - h * items;
-      turn_item<T, IL, VEC>((const T*)x.x + (t0 + t) * x.x_token + (h0 + h) * x.x_head,
-                            (T*)x.out + (t0 + t) * x.o_token + (h0 + h) * x.o_head, item, r.half, cs + t * r.half);
-    }
+    for (Walk w(h1 - h0, items); w.t < m; w.next())
+      turn_item<T, IL, VEC>((const T*)x.x + (t0 + w.t) * x.x_token + (h0 + w.row) * x.x_head,
+                            (T*)x.out + (t0 + w.t) * x.o_token + (h0 + w.row) * x.o_head, w.item, r.half,
+                            cs + w.t * r.half);
   }
 }
 
@@ -113,15 +137,15 @@ __global__ __launch_bounds__(256) void append_kernel(TokenCacheArgs c, RopeArgs 
   __shared__ float2 cs[kPairs];
   constexpr int V = 16 / sizeof(T);
   const int items = row_items<T, IL, VEC>(c.D, r.half), vch = c.D / V;
-  const int per_row = items + vch + 1, per_tok = c.G * per_row;
+  const int per_row = items + vch + 1;
   const int64_t tokens = (int64_t)c.B * a.n;
   for (int64_t t0 = (int64_t)blockIdx.x * nt; t0 < tokens; t0 += (int64_t)gridDim.x * nt) {
     const int m = (int)min((int64_t)nt, tokens - t0);
     __syncthreads();
     fill_angles(r, t0, m, cs);
     __syncthreads();
-    for (int i = threadIdx.x; i < m * per_tok; i += 256) {
-      const int t = i / per_tok, rem = i - t * per_tok, g = rem / per_row, item = rem - g * per_row;
+    for (Walk w(c.G, per_row); w.t < m; w.next()) {
+      const int t = w.t, g = w.row, item = w.item;
       const int64_t tok = t0 + t;
       const int b = (int)(tok / a.n), j = (int)(tok - (int64_t)b * a.n);
       const int p = a.pos[tok], slot = a.slots[((int64_t)b * c.G + g) * a.n + j];
