@@ -1022,12 +1022,36 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
   u32x4 qr[NV];
   float l2r = 0.f;
   uint32_t limr = 0;
-  auto load = [&](int64_t t) __attribute__((always_inline)) {
+  // Where this thread's chunks of the next tile lie: head and address of each, carried on by
+  // RT rows a tile (4096 tokens x 4 heads, 8 groups, 16384 slots, 128 dims: 686 us; with
+  // the products of rows and strides in every tile 726).
+  const int d_tok = token_of(a, RT), d_head = RT - d_tok * a.rep;
+  const int64_t step = d_tok * a.qs[1] + d_head * a.qs[2], wrap = a.qs[1] - a.rep * a.qs[2];
+  int head[NV];
+  const T* qp[NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int idx = j * 256 + tid, ch = idx % TL::CPR;
-      const int r = min((int)t * RT + idx / TL::CPR, (int)R - 1), i = token_of(a, r);
-      qr[j] = *reinterpret_cast<const u32x4*>(qbase + i * a.qs[1] + (r - i * a.rep) * a.qs[2] + ch * TL::EPC);
+  for (int j = 0; j < NV; ++j) {
+    const int idx = j * 256 + tid, r = (int)t0 * RT + idx / TL::CPR, i = token_of(a, r);
+    head[j] = r - i * a.rep;
+    qp[j] = qbase + i * a.qs[1] + head[j] * a.qs[2] + idx % TL::CPR * TL::EPC;
+  }
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
+    if ((t + 1) * RT <= R) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        qr[j] = *reinterpret_cast<const u32x4*>(qp[j]);
+        head[j] += d_head;
+        const bool c = head[j] >= a.rep;
+        head[j] -= c ? a.rep : 0;
+        qp[j] += step + (c ? wrap : 0);
+      }
+    } else {  // the last tile repeats the last row
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int idx = j * 256 + tid, ch = idx % TL::CPR;
+        const int r = min((int)t * RT + idx / TL::CPR, (int)R - 1), i = token_of(a, r);
+        qr[j] = *reinterpret_cast<const u32x4*>(qbase + i * a.qs[1] + (r - i * a.rep) * a.qs[2] + ch * TL::EPC);
+      }
     }
     if (tid < RT) {
       const int64_t r = t * RT + tid;
