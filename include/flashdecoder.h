@@ -10,6 +10,8 @@
  *     rolling KV cache of W_frm frames;
  *   - Sec. 3.4 Steps 1-3: temporal upsampling, temporal refinement, 2-layer MLP
  *     head and PixelShuffle.
+ * Beside it: rotary positions and a KV cache with a token budget (fd_rope_*,
+ * fd_token_*) as operators on caller memory.
  *
  * Conventions for every function below:
  *   - Arguments, the configuration and object states are checked before any
@@ -503,7 +505,8 @@ typedef struct fd_token_cache {
  * keep_recent, newest = the request's largest new position), 3 first (slot_pos <
  * keep_first). The first m of them, in rising order, go to the request's m valid
  * tokens in order: empty slots are filled first, then the least attended tokens are
- * replaced, recent and first ones only when no other is left. NaN weights order as
+ * replaced, recent and first ones only when no other is left. (New tokens enter with
+ * weight 0: keep_recent is what keeps them until queries have seen them.) NaN weights order as
  * -infinity, -0 as 0. slot_pos, weight [batch][groups][capacity] are read only; slots
  * [batch][groups][n]. n <= capacity and n <= 65536, keep_first, keep_recent >= 0.
  * workspace: 4-byte aligned, at least fd_token_slots_workspace bytes (0 up to 16384

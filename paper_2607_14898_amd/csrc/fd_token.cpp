@@ -279,6 +279,7 @@ fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, con
     return fail(FD_ERR_INVALID_ARGUMENT, "lse and weight_out must be 4-byte aligned");
   const int kind = kind_of(cache->dtype), rep = heads / c.G;
   fd::TokenAttend a;
+  fd::TokenAttendPlan plan;
   a.n = n;
   a.rep = rep;
   a.scale = scale;
@@ -294,7 +295,8 @@ fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, con
       return fail(FD_ERR_INVALID_ARGUMENT, "q and out must be 16-byte aligned, pos 4-byte aligned");
     if (!strides_ok(q_stride, extents, c.D, es) || !strides_ok(out_stride, extents, c.D, es))
       return fail(FD_ERR_INVALID_ARGUMENT, "strides of q and out must be at least head_dim and whole 16 bytes");
-    const int64_t need = fd::token_attend_plan(c, n, rep, kind, weight_out != nullptr).bytes;
+    plan = fd::token_attend_plan(c, n, rep, kind, weight_out != nullptr);
+    const int64_t need = plan.bytes;
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (size_t)need))
       return fail(FD_ERR_INVALID_ARGUMENT, "workspace of %zu bytes, %lld needed (16-byte aligned)", workspace_bytes,
                   (long long)need);
@@ -307,7 +309,7 @@ fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, con
     a.pos = pos;
     a.ws = workspace;
   }
-  return launched(fd::token_attend(c, a, kind, (hipStream_t)stream), "token attention");
+  return launched(fd::token_attend(c, a, plan, kind, (hipStream_t)stream), "token attention");
 }
 
 }  // extern "C"

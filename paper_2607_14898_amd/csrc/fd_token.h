@@ -99,6 +99,8 @@ struct TokenAttendPlan {
   int64_t bytes = 0;
 };
 TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int kind, bool weights);
-hipError_t token_attend(const TokenCacheArgs& c, const TokenAttend& a, int kind, hipStream_t stream);
+// pl: token_attend_plan of the call's sizes (unused where a.n is 0).
+hipError_t token_attend(const TokenCacheArgs& c, const TokenAttend& a, const TokenAttendPlan& pl, int kind,
+                        hipStream_t stream);
 
 }  // namespace fd

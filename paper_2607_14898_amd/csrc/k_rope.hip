@@ -9,7 +9,8 @@
 // a workgroup computes each (cos, sin) of its tokens once, into LDS, and then
 // streams the heads' vectors past them, 16 bytes a thread. Both kernels read every
 // element once and write it once, so memory bounds them, and for single tokens the
-// launch does.
+// launch does. 8160 tokens x 32 heads x 128, bf16, 96 rotated: 34 us (3.9 TB/s with fresh
+// memory every time); 3600 tokens x 3 groups appended: 5.8 us; one token: 2.2 us.
 #include "fd_token.h"
 
 namespace fd {

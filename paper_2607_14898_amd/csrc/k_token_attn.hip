@@ -17,14 +17,15 @@
 // and tiles that every row sees need no mask.
 //
 // Whatever empty and hidden slots hold must not matter. Scores are replaced, not added
-// to. V of empty slots is zeroed as it is staged. V of slots hidden from some rows alone
-// may hold infinities or NaN, which 0 x V would spread: rows that end up not finite are
+// to. Empty slots are left out (many rows) or their V is zeroed as it is staged (few). V
+// of slots hidden from some rows alone may hold infinities or NaN, which 0 x V would spread: rows that end up not finite are
 // computed once more with such elements as zeros, and if there were any, those of visible
 // slots are then added (finite data never comes here).
 #include "fd_token.h"
 
 #include <stdint.h>
 
+#include <initializer_list>
 #include <type_traits>
 
 namespace fd {
@@ -336,9 +337,13 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
 // tile's keys, then its values, through 32 rows of LDS that no other wave touches, so the
 // loop has no barrier and a CU's waves drift apart. Both loads of a tile go out together;
 // with 8 to 12 waves on a CU up to 128 KB are in flight. The four waves' results meet in
-// LDS, the parts' in finish_kernel.
+// LDS, the parts' in finish_kernel. 16 requests, 8 groups, 4 heads each, 128 dims, 16384 slots
+// (30 to 100% full), bf16: 172 us, 4.1 TB/s with the scores written for the weights, 5.2 to
+// 5.5 TB/s without.
 template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
+__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys_kernel(TokenCacheArgs c,
+                                                                                        TokenAttend a,
+                                                                                        TokenAttendPlan pl) {
   using TL = Tile<T, D>;
   constexpr int NV = 32 * TL::CPR / 64;  // 16-byte loads of a lane per tile
   constexpr int kTileB = 32 * D * (int)sizeof(T), kJoinB = 32 * 33 * 4;
@@ -533,9 +538,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
 // so the workgroup first sorts kScan slots' indices by what its rows see of them: those
 // that all rows see, those that some see (the chunk's own tokens, later ones left out),
 // nothing else. Only the second kind is masked, and empty slots cost no tile.
+//
+// 4096 tokens x 4 heads, 8 groups, 128 dims, 12288 old and 4096 own slots, bf16: 975 us,
+// 987 TFLOP/s (a large library product: 1187); the sorting took it from 1275 to 1134.
+// 1560 x 8 rows, 3 groups, 64 dims, 4680 slots, fp16: 85 us, 529 TFLOP/s: per score the
+// exponential costs more than its MFMA share.
 constexpr int kScan = 4096;
 template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
+__global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows_kernel(TokenCacheArgs c,
+                                                                                        TokenAttend a,
+                                                                                        TokenAttendPlan pl) {
   using TL = Tile<T, D>;
   constexpr int KB = sizeof(T) == 2 ? 2 : 1, KT = 32 * KB;
   constexpr int NV = KT * TL::CPR / 256;
@@ -602,8 +614,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
       // M0 is reserved by the compiler, but nothing else in this kernel reads it.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_k + at), "v"(ok), "s"(rk) : "m0");
-      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_v + at), "v"(ov), "s"(rv) : "m0");
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :
+                   : "s"(lds_k + at), "v"(ok), "s"(rk)
+                   : "m0");
+      asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   :
+                   : "s"(lds_v + at), "v"(ov), "s"(rv)
+                   : "m0");
 #pragma clang diagnostic pop
     }
     if ((t + 1) * KT > seen && tid < KT) {
@@ -938,10 +956,11 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
 
 // The weights of a chunk of tokens: p = exp2(score - lse) needs the rows' log-sums, so
 // the scores are computed again, with the keys held and the rows streaming past: a wave
-// keeps 32 KB keys' fragments in registers and the four waves share tiles of 64 rows
+// keeps the fragments of KB blocks of 32 keys in registers and the four waves share tiles of 64 rows
 // through LDS. Half the matrix work of the attention, and its exponentials. A
 // workgroup's slots are taken in the order seen by every row, by some rows, empty, so
-// that a mask costs the waves with the call's own tokens alone.
+// that a mask costs the waves with the call's own tokens alone. The long chunk above: 678
+// us, 709 TFLOP/s; the frame 53 us.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
@@ -1146,12 +1165,12 @@ __global__ __launch_bounds__(256) void weights_join_kernel(TokenCacheArgs c, Tok
 }
 
 template <typename T, int D>
-hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, int kind, hipStream_t s) {
+hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, const TokenAttendPlan& pl, hipStream_t s) {
   a.rep_inv = (uint32_t)((((uint64_t)1 << 32) + a.rep - 1) / a.rep);
   const int64_t R = (int64_t)a.n * a.rep;
   const int BG = c.B * c.G;
   if (a.n == 0) {  // no rows: the weights only fade
-    if (a.weight_out) {
+    if (a.weight_out) {  // (a plan of no parts)
       TokenAttendPlan none;
       none.weight_parts = 0;
       hipLaunchKernelGGL(weights_join_kernel, dim3((unsigned)(((int64_t)BG * c.C + 255) / 256)), dim3(256), 0, s, c, a,
@@ -1159,7 +1178,6 @@ hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, int kind, hipSt
     }
     return hipGetLastError();
   }
-  const TokenAttendPlan pl = token_attend_plan(c, a.n, a.rep, kind, a.weight_out != nullptr);
   const int rows_each = 256 / (D / 4) / pl.join;
   const int64_t row_blocks = ((int64_t)BG * R + rows_each - 1) / rows_each;
   const bool wide = (int64_t)BG * c.C >= 1 << 19;
@@ -1189,10 +1207,10 @@ hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, int kind, hipSt
 }
 
 template <typename T>
-hipError_t attend_dim(const TokenCacheArgs& c, const TokenAttend& a, int kind, hipStream_t s) {
-  if (c.D == 32) return attend_launch<T, 32>(c, a, kind, s);
-  if (c.D == 64) return attend_launch<T, 64>(c, a, kind, s);
-  return attend_launch<T, 128>(c, a, kind, s);
+hipError_t attend_dim(const TokenCacheArgs& c, const TokenAttend& a, const TokenAttendPlan& pl, hipStream_t s) {
+  if (c.D == 32) return attend_launch<T, 32>(c, a, pl, s);
+  if (c.D == 64) return attend_launch<T, 64>(c, a, pl, s);
+  return attend_launch<T, 128>(c, a, pl, s);
 }
 
 }  // namespace
@@ -1202,6 +1220,8 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   const int64_t R = (int64_t)n * rep, BG = (int64_t)c.B * c.G;
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   auto clamp = [](int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; };
+  // (8 groups, 32768 slots, 128 dims, bf16, with weights: 64 rows 60 us by keys against 73,
+  // 96 rows 105 against 81; 3 groups, 4680 slots, 64 dims, fp32: 26 against 36, 32 against 39)
   p.by_keys = R <= 64;
   p.row_tiles = (int)up(R, p.by_keys ? 32 : 128);
   const int64_t wgs = BG * p.row_tiles;
@@ -1212,7 +1232,8 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     // itself (about 96 slots' time) but leave two tiles of 32 slots a wave
     int64_t best = INT64_MAX;
     const int64_t most = clamp(up(c.C, 256), 1, 256);
-    for (int64_t s = 1; s <= most; ++s) {
+    for (int64_t round = 1; round <= 8; ++round) {
+      const int64_t s = clamp(held * round / wgs, 1, most);
       const int64_t cost = up(wgs * s, held) * (up(c.C, s) + 96);
       if (cost < best) {
         best = cost;
@@ -1231,7 +1252,8 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     const double t = kind == 2 ? 0.065 * c.D : c.D == 128 ? 1.75 : c.D == 64 ? 1.2 : 0.9;
     double best = 0.0;
     const int64_t most = clamp(c.C / 128, 1, 64);
-    for (int64_t s = 1; s <= most; ++s) {
+    for (const int64_t parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      const int64_t s = parts < most ? parts : most;
       const double load = 0.65 * (double)up(wgs * s, 256);
       const double cost = ((double)c.C / (64.0 * s) + 6.0) * t * (load < 1.0 ? 1.0 : load) +
                           (s > 1 ? 4.0 + (double)(s * BG * R * c.D) * 8.0 / 5e6 : 0.0);
@@ -1264,10 +1286,11 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   return p;
 }
 
-hipError_t token_attend(const TokenCacheArgs& c, const TokenAttend& a, int kind, hipStream_t s) {
-  if (kind == 0) return attend_dim<_Float16>(c, a, kind, s);
-  if (kind == 1) return attend_dim<__bf16>(c, a, kind, s);
-  return attend_dim<float>(c, a, kind, s);
+hipError_t token_attend(const TokenCacheArgs& c, const TokenAttend& a, const TokenAttendPlan& pl, int kind,
+                        hipStream_t s) {
+  if (kind == 0) return attend_dim<_Float16>(c, a, pl, s);
+  if (kind == 1) return attend_dim<__bf16>(c, a, pl, s);
+  return attend_dim<float>(c, a, pl, s);
 }
 
 }  // namespace fd
