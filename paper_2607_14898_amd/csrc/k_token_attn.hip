@@ -373,26 +373,27 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   const T* vb = (const T*)c.v + b * c.vs[0] + g * c.vs[1];
   const int* ps = c.pos + (int64_t)bg * c.C;
 
-  const int tiles = (c.C + 31) / 32, per = (tiles + pl.splits - 1) / pl.splits;
-  const int t0 = split * per + wave, t1 = min(tiles, (split + 1) * per);
+  // Tiles are dealt to the parts' waves in turn: used slots lie in front in a cache that has
+  // room, and contiguous parts behind them would have nothing to do.
+  const int tiles = (c.C + 31) / 32, hop = 4 * pl.splits, t0 = 4 * split + wave;
   u32x4* tile = buf[wave];
   Softmax<T, D, true> sx;
   bool changed = false;  // some value of this wave's slots is not finite
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
-    for (int tc = t0; tc < t1; tc += 4 * 64) {
+    for (int tc = t0; tc < tiles; tc += hop * 64) {
       // which of the wave's next 64 tiles any row sees, two tiles a load: walked one by one,
       // an empty tile would cost a wait for memory
       uint64_t live = 0;
 #pragma unroll 8
       for (int x = 0; x < 32; ++x) {
-        const int t = tc + 4 * (2 * x + lh), sp = t * 32 + lr;
-        const uint64_t m = __ballot((t < t1 && sp < c.C ? (uint32_t)ps[sp] : ~0u) < lim_max);
+        const int t = tc + hop * (2 * x + lh), sp = t * 32 + lr;
+        const uint64_t m = __ballot((t < tiles && sp < c.C ? (uint32_t)ps[sp] : ~0u) < lim_max);
         live |= (uint64_t)((uint32_t)m != 0) << (2 * x) | (uint64_t)((uint32_t)(m >> 32) != 0) << (2 * x + 1);
-        if (tc + 8 * (x + 1) >= t1) break;
+        if (tc + 2 * hop * (x + 1) >= tiles) break;
       }
       while (live) {
-        const int t = tc + 4 * __builtin_ctzll(live);
+        const int t = tc + hop * __builtin_ctzll(live);
         live &= live - 1;
         const int p = t * 32 + lr < c.C ? ps[t * 32 + lr] : -1;
         const uint32_t taken = (uint32_t)__ballot(p >= 0);
@@ -455,7 +456,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
     }
     if (scrub) {
       if (__ballot(changed))
-        for (int t = t0; t < t1; t += 4)
+        for (int t = t0; t < tiles; t += hop)
           sx.add_unbounded(vb, c.vs[2], ps, t * 32, min(t * 32 + 32, c.C), w.lim, lane);
       break;
     }
@@ -543,7 +544,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
 // 987 TFLOP/s (a large library product: 1187); the sorting took it from 1275 to 1134.
 // 1560 x 8 rows, 3 groups, 64 dims, 4680 slots, fp16: 85 us, 529 TFLOP/s: per score the
 // exponential costs more than its MFMA share.
-constexpr int kScan = 4096;
+constexpr int kScan = 4096, kBlock = 64;
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows_kernel(TokenCacheArgs c,
                                                                                         TokenAttend a,
@@ -593,8 +594,10 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   const uint32_t wg_lim = max(max(slim[0][0], slim[0][1]), max(slim[0][2], slim[0][3]));
   const uint32_t wg_min = min(wg_lim, min(min(slim[1][0], slim[1][1]), min(slim[1][2], slim[1][3])));
 
-  const int per = (c.C + pl.splits - 1) / pl.splits;
-  const int s_lo = split * per, s_hi = min(c.C, s_lo + per);
+  // Blocks of kBlock slots are dealt to the parts in turn (used slots lie in front in a
+  // cache that has room). Place l of a scan is slot c0 + l + (l / kBlock) skip.
+  const int skip = kBlock * (pl.splits - 1), span = pl.scan * pl.splits;
+  auto from_c0 = [&](uint32_t l) { return __umul24(l / kBlock, (uint32_t)skip) + l; };
   const uint32_t kstep = (uint32_t)c.ks[2] * sizeof(T), vstep = (uint32_t)c.vs[2] * sizeof(T);  // below 2^24
   const uint32_t lds_k = lds_address(&sk[0][0]), lds_v = lds_address(&sv[0][0]);
   auto pos_of = [&](int s) { return *(const int*)((const char*)ps + 4u * (uint32_t)s); };
@@ -607,7 +610,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int idx = j * 256 + tid, r = idx / TL::CPR, e = t * KT + r;
-      const uint32_t s = list[min(e, m - 1)];
+      const uint32_t s = from_c0(list[min(e, m - 1)]);
       const uint32_t ok = __umul24(s, kstep) + 16 * (TL::k(r, idx % TL::CPR) - r * TL::CPR);
       const uint32_t ov = __umul24(s, vstep) + 16 * (TL::v(r, idx % TL::CPR) - r * TL::CPR);
       const uint32_t at = 16u * (uint32_t)(buf * KT * TL::CPR + j * 256 + wave * 64);
@@ -626,7 +629,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     }
     if ((t + 1) * KT > seen && tid < KT) {
       const int e = t * KT + tid;
-      pr = e < m ? pos_of(c0 + list[e]) : -1;
+      pr = e < m ? pos_of(c0 + (int)from_c0(list[e])) : -1;
     }
   };
   // the DMA of tile t is complete and its readers may begin, those of the one before are done
@@ -650,11 +653,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   Softmax<T, D, false> sx;
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
-    for (c0 = s_lo; c0 < s_hi; c0 += pl.scan) {
-      const int c1 = min(s_hi, c0 + pl.scan);
+    for (c0 = split * kBlock; c0 < c.C; c0 += span) {
+      const int c1 = min(c.C, c0 + span);
       auto scanned = [&](int x) {
-        const int s = c0 + wave * (kScan / 4) + x * 64 + lane;
-        return (uint32_t)(s < c1 ? pos_of(s) : -1);
+        const int l = wave * (kScan / 4) + x * 64 + lane, s = c0 + (int)from_c0((uint32_t)l);
+        return (uint32_t)(l < pl.scan && s < c1 ? pos_of(s) : -1);
       };
       int n0 = 0, n1 = 0;
 #pragma unroll 8
@@ -736,7 +739,9 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
     }
     __syncthreads();
     if (scrub) {
-      if (schanged) sx.add_unbounded(vbase, c.vs[2], ps, s_lo, s_hi, w.lim, lane);
+      if (schanged)
+        for (int s = split * kBlock; s < c.C; s += kBlock * pl.splits)
+          sx.add_unbounded(vbase, c.vs[2], ps, s, min(s + kBlock, c.C), w.lim, lane);
       break;
     }
     if (!__syncthreads_or(w.lim != 0 && !sx.finite())) break;
@@ -1020,6 +1025,17 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
       lslot[at] = min(s, c.C - 1);
       lpos[at] = p;
     }
+    int used = 0;
+    for (int x = 0; x < 2; ++x)
+      for (int w = 0; w < 4; ++w) used += scount[x][w];
+    if (used == 0) {  // (the whole workgroup)
+      if (tid < KW && s < c.C) {
+        if (pl.weight_parts > 1)
+          ((float*)a.ws)[pl.weights + ((int64_t)bg * pl.weight_parts + part) * c.C + s] = 0.f;
+        else a.weight_out[(int64_t)bg * c.C + s] = 0.f;
+      }
+      return;
+    }
   }
   __syncthreads();
 
@@ -1241,9 +1257,9 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
       }
     }
   } else {
-    // slots whose byte offsets from the first fit 32 bits
+    // byte offsets of a scan's slots from its first fit 32 bits
     const int64_t step = (kind == 2 ? 4 : 2) * (c.ks[2] > c.vs[2] ? c.ks[2] : c.vs[2]);
-    p.scan = (int)clamp(((int64_t)1 << 32) / (step > 0 ? step : 1) / 64 * 64 - 64, 64, kScan);
+    const int64_t blocks = ((int64_t)1 << 32) / ((c.C > 1 && step > 0 ? step : 1) * kBlock);  // >= 4
     // Parts by a model of what was measured, in us: a tile of 64 slots takes a workgroup
     // alone on its CU t, L of them on one CU 0.65 L t, a workgroup's ends six tiles' time, and
     // joining parts a launch and its traffic. (1560 tokens x 8 heads, 3 groups, 4680 slots, 64
@@ -1251,7 +1267,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     // fp32: two parts 64 us, eleven 21.) More parts only where they gain 5%.
     const double t = kind == 2 ? 0.065 * c.D : c.D == 128 ? 1.75 : c.D == 64 ? 1.2 : 0.9;
     double best = 0.0;
-    const int64_t most = clamp(c.C / 128, 1, 64);
+    const int64_t most = clamp(c.C / kBlock, 1, blocks < 64 ? blocks : 64);
     for (const int64_t parts : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       const int64_t s = parts < most ? parts : most;
       const double load = 0.65 * (double)up(wgs * s, 256);
@@ -1262,6 +1278,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
         p.splits = (int)s;
       }
     }
+    p.scan = (int)clamp(blocks / p.splits, 1, kScan / kBlock) * kBlock;
     const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
     p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
   }
