@@ -338,7 +338,7 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
 // loop has no barrier and a CU's waves drift apart. Both loads of a tile go out together;
 // with 8 to 12 waves on a CU up to 128 KB are in flight. The four waves' results meet in
 // LDS, the parts' in finish_kernel. 16 requests, 8 groups, 4 heads each, 128 dims, 16384 slots
-// (30 to 100% full), bf16: 172 us, 4.1 TB/s with the scores written for the weights, 5.2 to
+// (30 to 100% full), bf16: 168 us, 4.2 TB/s with the scores written for the weights, 5.2 to
 // 5.5 TB/s without.
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys_kernel(TokenCacheArgs c,

@@ -364,3 +364,47 @@ def test_stream(dtype):
     cache.reset()
     out, lse = cache.attend(qr, pos)
     assert not out.any() and not cache.weight.any()
+
+
+@pytest.mark.parametrize("C,n", [(300, 1), (300, 40), (20000, 30)])
+def test_captured_step(C, n):
+    """insert and attend of one step captured into a graph and replayed on changing inputs, against eager steps of a
+    twin cache; the state goes on from replay to replay."""
+    B, G, N, D = 2, 2, 8, 64
+    gen = torch.Generator().manual_seed(C + n)
+    rope = fdb.Rope(fdb.fd_rope_frequencies(D)[0])
+    first = make(B, G, N, D, 4, C, BF16, seed=8)
+    twins = [fdb.TokenCache(*(t.clone() for t in first[:4])) for _ in range(2)]
+    k, v, q = (torch.zeros(B, n, h, D, dtype=BF16, device="cuda") for h in (G, G, N))
+    pos = torch.zeros(B, n, dtype=torch.int32, device="cuda")
+
+    def step(cache):
+        slots = cache.insert(k, v, pos, rope=rope, keep_first=4, keep_recent=n + 8)
+        qr = rope(q.view(B * n, N, D), pos.view(-1)).view(B, n, N, D)
+        return (slots, *cache.attend(qr, pos, decay=0.95))
+
+    def fill(i):
+        for t in (k, v, q):
+            t.copy_(torch.randn(t.shape, generator=gen).to(BF16))
+        pos.copy_((2 * C + i * n + torch.arange(n, dtype=torch.int32)).expand(B, n))
+        if n > 1:
+            pos[1, n // 2] = -1
+
+    fill(0)
+    side = torch.cuda.Stream()  # (the first calls of a process load code: not under capture)
+    with torch.cuda.stream(side):
+        step(fdb.TokenCache(*(t.clone() for t in first[:4])))
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(twins[1])
+    for i in range(1, 5):
+        fill(i)
+        want = step(twins[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+        for name in ("k", "v", "pos", "weight"):
+            assert torch.equal(getattr(twins[1], name), getattr(twins[0], name))
+    assert bool((twins[0].pos >= 0).all())
