@@ -93,6 +93,7 @@ struct TokenAttendPlan {
   int splits = 1;       // parts of the slots
   int scan = 1;         // slots that a workgroup sorts at a time (not by_keys)
   int weight_parts = 1; // parts of the rows in the pass over the weights
+  int row_waves = 1;    // waves that share keys in that pass
   int join = 1;         // groups of threads that share a row's parts when they are joined
   // offsets into the workspace, in floats
   int64_t part_o = 0, part_ml = 0, lse2 = 0, scores = 0, weights = 0;

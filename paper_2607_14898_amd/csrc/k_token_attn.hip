@@ -964,13 +964,15 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
 // keeps the fragments of KB blocks of 32 keys in registers and the four waves share tiles of 64 rows
 // through LDS. Half the matrix work of the attention, and its exponentials. A
 // workgroup's slots are taken in the order seen by every row, by some rows, empty, so
-// that a mask costs the waves with the call's own tokens alone. The long chunk above: 678
+// that a mask costs the waves with the call's own tokens alone. Where whole workgroups would
+// leave CUs idle, RW = 2 waves share their keys and take every other 32 rows (61 tokens x 4
+// heads, 6 groups, 1531 slots, fp32: 15 us against 19.5). The long chunk above: 678
 // us, 709 TFLOP/s; the frame 53 us.
-template <typename T, int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
+template <typename T, int D, int RW>
+__global__ __launch_bounds__(256, D == 128 || RW == 2 ? 2 : 3) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
   constexpr int KB = sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a wave
-  constexpr int KW = 128 * KB;                // slots of a workgroup
+  constexpr int KW = 128 * KB / RW;           // slots of a workgroup
   constexpr int RT = 64;                      // rows of a tile
   constexpr int NV = RT * TL::CPR / 256;
   __shared__ u32x4 sq[2][RT * TL::CPR];
@@ -980,8 +982,10 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
   __shared__ uint32_t lpos[KW];   // and their positions (empty: from 2^31 on)
   __shared__ uint32_t smin;
   __shared__ int scount[3][4];
+  __shared__ float spart[4 / RW][KB][16][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
+  const int kwave = wave / RW, rwave = wave % RW;
   const int slot_blocks = (c.C + KW - 1) / KW;
   const int kbk = blockIdx.x % slot_blocks, part = blockIdx.x / slot_blocks;
   const int bg = blockIdx.y, b = bg / c.G, g = bg - b * c.G;
@@ -1043,7 +1047,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
   uint32_t p_max = 0, p_min = ~0u;
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
-    const int at = (wave * KB + kb) * 32 + lr;
+    const int at = (kwave * KB + kb) * 32 + lr;
     const uint32_t p = lpos[at];
     p_max = p < 0x80000000u ? max(p_max, p) : p_max;  // (what empty slots add up is not stored)
     p_min = min(p_min, p);
@@ -1119,7 +1123,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
     const int cur = (int)(t - t0) & 1;
     if (t + 1 < t1) load(t + 1);
 #pragma unroll 1
-    for (int rb = 0; rb < RT / 32; ++rb) {
+    for (int rb = rwave; rb < RT / 32; rb += RW) {
       const uint32_t lim = slim[cur][32 * rb + lr];
       if (__ballot(lim > p_min) == 0) continue;
       const bool all = __ballot(lim > p_max) == ~0ull;
@@ -1145,7 +1149,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const uint32_t p = lpos[(wave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)];
+            const uint32_t p = lpos[(kwave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3)];
             const float x = __builtin_amdgcn_exp2f(fmaf(s[kb][r], cs, nl));
             sum[kb][r] += p < lim ? x : 0.f;
           }
@@ -1154,13 +1158,26 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void weights_kernel(TokenCac
     if (t + 1 < t1) stage(cur ^ 1);
     __syncthreads();
   }
-  // over the 32 rows of a half
+  // over the 32 rows of a half, then over the waves that shared the rows
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum[kb][r] = half_sum(sum[kb][r]);
+  if constexpr (RW > 1) {
+    if (rwave == 1 && lr == 31)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) spart[kwave][kb][r][lh] = sum[kb][r];
+    __syncthreads();
+    if (rwave == 1) return;
+  }
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float x = half_sum(sum[kb][r]);
-      const int at = (wave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+      const float x = RW > 1 ? sum[kb][r] + spart[kwave][kb][r][lh] : sum[kb][r];
+      const int at = (kwave * KB + kb) * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
       // (the list's end repeats no slot: a last, short block leaves its surplus out)
       if (lr == 31 && at < min(KW, c.C - kbk * KW)) {
         const int64_t s = lslot[at], slot = (int64_t)bg * c.C + s;
@@ -1212,9 +1229,10 @@ hipError_t attend_launch(const TokenCacheArgs& c, TokenAttend a, const TokenAtte
                      pl);
   if (pl.splits > 1) finish(false);
   if (a.weight_out) {
-    constexpr int KW = sizeof(T) == 2 ? 256 : 128;
-    hipLaunchKernelGGL((weights_kernel<T, D>), dim3((unsigned)((c.C + KW - 1) / KW * pl.weight_parts), (unsigned)BG),
-                       dim3(256), 0, s, c, a, pl);
+    const int kw = (sizeof(T) == 2 ? 256 : 128) / pl.row_waves;
+    const dim3 grid((unsigned)((c.C + kw - 1) / kw * pl.weight_parts), (unsigned)BG);
+    if (pl.row_waves == 2) hipLaunchKernelGGL((weights_kernel<T, D, 2>), grid, dim3(256), 0, s, c, a, pl);
+    else hipLaunchKernelGGL((weights_kernel<T, D, 1>), grid, dim3(256), 0, s, c, a, pl);
     if (pl.weight_parts > 1)
       hipLaunchKernelGGL(weights_join_kernel, dim3((unsigned)(((int64_t)BG * c.C + 255) / 256)), dim3(256), 0, s, c, a,
                          pl);
@@ -1281,6 +1299,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     p.scan = (int)clamp(blocks / p.splits, 1, kScan / kBlock) * kBlock;
     const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
     p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
+    p.row_waves = p.weight_parts == 1 && kw * 2 <= held ? 2 : 1;
   }
   int64_t at = 0;
   auto take = [&](int64_t floats) {
