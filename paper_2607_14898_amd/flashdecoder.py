@@ -548,11 +548,19 @@ def _call_on(device, stream, fn, *args) -> None:
         _check(st)
 
 
-def _new(like, shape, dtype, stream):
-    """An uninitialised tensor on like's GPU that work on `stream` may use until it is done."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
+def _new(like, shape, dtype, stream, result: bool = True):
+    """An uninitialised tensor on like's GPU for work on `stream` (None: the current one),
+    out of that stream's memory: what the current one last freed, its work may still use.
+    A result also stays until the current stream's work at its release is done."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    import torch
+    if stream.device != like.device:
+        raise ValueError(f"stream of {stream.device} for tensors on {like.device}")
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    if result:
+        t.record_stream(torch.cuda.current_stream(like.device))
     return t
 
 
@@ -630,7 +638,7 @@ def fd_token_slots_device(slot_pos, weight, pos, slots, keep_first: int = 0, kee
         b = ctypes.c_size_t()
         _check(lib.fd_token_slots_workspace(B, G, C, n, ctypes.byref(b)))
         size = b.value
-        ws = _new(slots, (size,), torch.uint8, stream)
+        ws = _new(slots, (size,), torch.uint8, stream, result=False)
     _call_on(dev, stream, lib.fd_token_slots_device, slot_pos.data_ptr(), weight.data_ptr(), B, G, C, pos.data_ptr(), n,
              keep_first, keep_recent, slots.data_ptr(), None if ws is None else ws.data_ptr(), size)
 
@@ -731,7 +739,7 @@ class TokenCache:
             b = ctypes.c_size_t()
             _check(lib.fd_token_attend_workspace(self._p, heads, n, int(key[2]), ctypes.byref(b)))
             size = self._ws[key] = b.value
-        ws = _new(q, (size,), torch.uint8, stream)
+        ws = _new(q, (size,), torch.uint8, stream, result=False)
         _call_on(dev, stream, lib.fd_token_attend_device, self._p, q.data_ptr(), I3(*q.stride()[:3]), heads, n,
                  pos.data_ptr(), D ** -0.5 if scale is None else scale, int(causal), out.data_ptr(),
                  I3(*out.stride()[:3]), lse.data_ptr(), decay,

@@ -308,6 +308,32 @@ def test_captured_and_side_streams(n):
         assert torch.equal(o, e[0]) and torch.equal(l, e[1]) and torch.equal(w, e[2])
 
 
+def test_memory_of_a_side_stream():
+    """Results and workspaces of another stream are not memory that the current one's work may still use."""
+    shape = (1, 256, 8, 64)
+    rope = fdb.Rope(fdb.fd_rope_frequencies(64)[0])
+    cache = fdb.TokenCache.empty(1, 2, 2048, 64, F16)
+    pos = torch.arange(256, dtype=torch.int32, device="cuda").view(1, -1)
+    x = torch.randn(*shape, device="cuda").to(F16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    freed = torch.empty_like(x).data_ptr()  # (handed out again for the same size)
+    assert torch.empty_like(x).data_ptr() == freed
+    turned = rope(x[0], pos[0], stream=side)
+    assert turned.data_ptr() != freed
+    out, _ = cache.attend(x, pos, track=False, stream=side)
+    assert out.data_ptr() != freed
+    side.synchronize()
+    assert torch.equal(turned, rope(x[0], pos[0])) and not out.any()
+    # a released result is not handed to its stream again before the current one's work is done
+    at = out.data_ptr()
+    torch.cuda._sleep(10 ** 7)
+    del out
+    again, _ = cache.attend(x, pos, track=False, stream=side)
+    assert again.data_ptr() != at
+    torch.cuda.synchronize()
+
+
 def test_frame_mask_of_the_decoder():
     """Frame indices as positions give the decoder's mask: a frame's tokens see each other and earlier frames."""
     L, frames = 30, 3
