@@ -543,8 +543,9 @@ fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, 
  * (0 for empty slots). Tokens with pos < 0 are padding and see nothing; a row that sees
  * nothing (or scores of -infinity alone) gives out 0 and lse -infinity and adds nothing
  * to the weights. Nothing that a row does not see reaches its results, infinities and NaN
- * included. A decoder's
- * frame mask is causal = 1 with the frame index as every token's position.
+ * included; an infinity or a NaN among the values that it sees does, however small its
+ * probability. A decoder's frame mask is causal = 1 with the frame index as every token's
+ * position.
  *   q, out      [batch][n][heads][head_dim] of the cache's dtype by strides (host arrays:
  *               batch, token, head; whole 16 bytes), rows 16-byte aligned, no overlap
  *   lse         [batch][heads][n] fp32, or NULL

@@ -324,6 +324,12 @@ template <typename T, int D, bool EXACT> struct Softmax {
   }
 };
 
+// A part's output on the joined shift. A factor that underflows takes a part out, but not
+// the infinities and NaN of values that the row sees: they reach it however slots are parted.
+__device__ __forceinline__ float on_shift(float x, float f) {
+  return f != 0.f ? x * f : isfinite(x) ? 0.f : x;
+}
+
 // Stores 4 consecutive dims.
 template <typename T> __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
   struct alignas(4 * sizeof(T)) Q { T e[4]; };
@@ -508,7 +514,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   for (int d = 0; d < D / 32; ++d) {
     float* so = (float*)buf[wave];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) so[lr * 33 + 8 * (r >> 2) + 4 * lh + (r & 3)] = f == 0.f ? 0.f : sx.acc[d][r] * f;
+    for (int r = 0; r < 16; ++r) so[lr * 33 + 8 * (r >> 2) + 4 * lh + (r & 3)] = on_shift(sx.acc[d][r], f);
     __syncthreads();
     float o[4];
 #pragma unroll
@@ -864,18 +870,17 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int64_t s = min(s0 + e * pl.join, S - 1);
-        ms[e] = s0 + e * pl.join < S ? ml[s * R].x : -INFINITY;
+        ms[e] = ml[s * R].x;
         p[e] = *reinterpret_cast<const float4*>(po + s * R * D);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        if (s0 + e * pl.join >= S) break;
         const float f = ms[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[e] - M);
-        if (f != 0.f) {  // (a part that saw nothing holds no number)
-          o.x = fmaf(f, p[e].x, o.x);
-          o.y = fmaf(f, p[e].y, o.y);
-          o.z = fmaf(f, p[e].z, o.z);
-          o.w = fmaf(f, p[e].w, o.w);
-        }
+        o.x += on_shift(p[e].x, f);
+        o.y += on_shift(p[e].y, f);
+        o.z += on_shift(p[e].z, f);
+        o.w += on_shift(p[e].w, f);
       }
     }
     if (pl.join > 1) {
