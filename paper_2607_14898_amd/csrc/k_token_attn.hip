@@ -20,7 +20,8 @@
 // to. Empty slots are left out (many rows) or their V is zeroed as it is staged (few). V
 // of slots hidden from some rows alone may hold infinities or NaN, which 0 x V would spread: rows that end up not finite are
 // computed once more with such elements as zeros, and if there were any, those of visible
-// slots are then added (finite data never comes here).
+// slots are then added. Finite data comes here only where its unnormalised sums overflow; the
+// second time they do not.
 #include "fd_token.h"
 
 #include <stdint.h>
@@ -38,12 +39,17 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Values of fp32's range may overflow the sums, whose probabilities reach 2^8 for up to 2^24
+// slots. Rows that end not finite are computed again, and then these are 2^-40 of that.
+constexpr float kBelow = 40.f;
+
 template <typename T> struct Op;
 template <> struct Op<_Float16> {
   using V = f16x8;
   // Probabilities are kept below 2^15 and, with the running maximum at 2^6, above the
   // subnormal f16 values down to 2^-20 of it.
   static constexpr float kShift = 6.f;
+  static constexpr float kDown = 0.f;  // (f16 values times those sums are far from fp32's end)
   static __device__ __forceinline__ f32x16 mma(V a, V b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
@@ -51,6 +57,7 @@ template <> struct Op<_Float16> {
 template <> struct Op<__bf16> {
   using V = bf16x8;
   static constexpr float kShift = 0.f;
+  static constexpr float kDown = kBelow;
   static __device__ __forceinline__ f32x16 mma(V a, V b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -58,6 +65,7 @@ template <> struct Op<__bf16> {
 template <> struct Op<float> {
   using V = f32x8;
   static constexpr float kShift = 0.f;
+  static constexpr float kDown = kBelow;
   static __device__ __forceinline__ f32x16 mma(V a, V b, f32x16 c) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
@@ -221,9 +229,10 @@ template <typename T, int D, bool EXACT> struct Softmax {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
   }
-  // Scores of KB 32-key blocks (hidden ones -inf) and their values in LDS.
+  // Scores of KB 32-key blocks (hidden ones -inf) and their values in LDS. Probabilities
+  // enter 2^-down of what the shift says.
   template <int KB>
-  __device__ __forceinline__ void add(f32x16 (&s)[KB], float c, const u32x4* vt, int row0, int lane) {
+  __device__ __forceinline__ void add(f32x16 (&s)[KB], float c, float down, const u32x4* vt, int row0, int lane) {
     float mx = s[0][0];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -242,7 +251,7 @@ template <typename T, int D, bool EXACT> struct Softmax {
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] *= f;
     }
-    const float sub = m == -INFINITY ? 0.f : O::kShift - m;
+    const float sub = m == -INFINITY ? 0.f : O::kShift - down - m;
     // 16 keys at a time where registers are short, else all the exponentials before all
     // the MFMAs (which then run at raised priority in one go)
     constexpr int NX = KB * 2, GX = D == 128 ? 1 : NX;
@@ -336,7 +345,7 @@ template <typename T> __device__ __forceinline__ void store4(T* p, float a, floa
   *reinterpret_cast<Q*>(p) = Q{(T)a, (T)b, (T)c, (T)d};
 }
 
-// (part_ml holds shift and sum of each part's rows, part_o their unnormalised output.)
+// (part_ml holds shift and sum of each part's rows, part_o their output.)
 
 // Few rows (serving): memory bounds it, so the keys are parted among as many waves as it
 // takes. A wave walks 32-slot tiles of its workgroup's part on its own: it stages a
@@ -454,13 +463,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        sx.template add<1>(s, cs, tile, 0, lane);
+        sx.template add<1>(s, cs, scrub ? Op<T>::kDown : 0.f, tile, 0, lane);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
       }
     }
     if (scrub) {
+      sx.m += Op<T>::kDown;
       if (__ballot(changed))
         for (int t = t0; t < tiles; t += hop)
           sx.add_unbounded(vb, c.vs[2], ps, t * 32, min(t * 32 + 32, c.C), w.lim, lane);
@@ -486,6 +496,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   float L = 0.f;
 #pragma unroll
   for (int x = 0; x < 4; ++x) L += sm[x][lr] == -INFINITY ? 0.f : sl[x][lr] * __builtin_amdgcn_exp2f(sm[x][lr] - M);
+  // (normalised before they are added up: sums of parts could overflow where their mean does not)
+  const float part = f == 0.f ? 0.f : f / L;
   const bool direct = pl.splits == 1 && !a.weight_out;
   float* ml = (float*)a.ws + pl.part_ml + (((int64_t)bg * pl.splits + split) * R + row) * 2;
   if (wave == 0 && lh == 0 && row < R) {
@@ -501,20 +513,12 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
   const int orow = tid >> 3, od = 4 * (tid & 7);
   const int64_t orow_g = (int64_t)rt * 32 + orow;
   const Row ow = row_of(a, b, g, orow_g, R);
-  float inv = 0.f;
-  {
-    const float oM = fmaxf(fmaxf(sm[0][orow], sm[1][orow]), fmaxf(sm[2][orow], sm[3][orow]));
-    float oL = 0.f;
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      oL += sm[x][orow] == -INFINITY ? 0.f : sl[x][orow] * __builtin_amdgcn_exp2f(sm[x][orow] - oM);
-    inv = oM == -INFINITY ? 0.f : 1.f / oL;
-  }
+  const bool none = fmaxf(fmaxf(sm[0][orow], sm[1][orow]), fmaxf(sm[2][orow], sm[3][orow])) == -INFINITY;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) {
     float* so = (float*)buf[wave];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) so[lr * 33 + 8 * (r >> 2) + 4 * lh + (r & 3)] = on_shift(sx.acc[d][r], f);
+    for (int r = 0; r < 16; ++r) so[lr * 33 + 8 * (r >> 2) + 4 * lh + (r & 3)] = on_shift(sx.acc[d][r], part);
     __syncthreads();
     float o[4];
 #pragma unroll
@@ -525,8 +529,8 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
     }
     if (orow_g < R) {
       if (direct) {
-        if (inv == 0.f) store4(out_of<T>(a, b, ow) + 32 * d + od, 0.f, 0.f, 0.f, 0.f);
-        else store4(out_of<T>(a, b, ow) + 32 * d + od, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        if (none) store4(out_of<T>(a, b, ow) + 32 * d + od, 0.f, 0.f, 0.f, 0.f);
+        else store4(out_of<T>(a, b, ow) + 32 * d + od, o[0], o[1], o[2], o[3]);
       } else {
         store4((float*)a.ws + pl.part_o + (((int64_t)bg * pl.splits + split) * R + orow_g) * D + 32 * d + od, o[0], o[1],
                o[2], o[3]);
@@ -738,13 +742,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
               for (int r = 0; r < 16; ++r)
                 if ((uint32_t)spos[cur][32 * kb + 16 * (r >> 3) + 8 * lh + (r & 7)] >= w.lim) s[kb][r] = -INFINITY;
           }
-          sx.template add<KB>(s, cs, sv[cur], 0, lane);
+          sx.template add<KB>(s, cs, scrub ? Op<T>::kDown : 0.f, sv[cur], 0, lane);
         }
         if (t + 1 < tiles) arrive(t + 1, cur ^ 1, scrub);
       }
     }
     __syncthreads();
     if (scrub) {
+      sx.m += Op<T>::kDown;
       if (schanged)
         for (int s = split * kBlock; s < c.C; s += kBlock * pl.splits)
           sx.add_unbounded(vbase, c.vs[2], ps, s, min(s + kBlock, c.C), w.lim, lane);
@@ -776,12 +781,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
       ml[0] = sx.m;
       ml[1] = L;
     }
+    const float inv = none ? 0.f : 1.f / L;
     float* o = (float*)a.ws + pl.part_o + pr_ * D;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        store4(o + 32 * d + 2 * r + 4 * lh_, sx.acc[d][r], sx.acc[d][r + 1], sx.acc[d][r + 2], sx.acc[d][r + 3]);
+        store4(o + 32 * d + 2 * r + 4 * lh_, on_shift(sx.acc[d][r], inv), on_shift(sx.acc[d][r + 1], inv),
+               on_shift(sx.acc[d][r + 2], inv), on_shift(sx.acc[d][r + 3], inv));
     return;
   }
   if (lh_ == 0) {
@@ -853,10 +860,10 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
     __shared__ float4 s_o[256];
     const int64_t rows = (int64_t)c.B * c.G * R;
     const int group = tid / TPR % pl.join;
-    const int64_t x_ = (int64_t)blockIdx.x * (RPB / pl.join) + tid / TPR / pl.join, x = min(x_, rows - 1);
+    const int64_t row_ = (int64_t)blockIdx.x * (RPB / pl.join) + tid / TPR / pl.join, row = min(row_, rows - 1);
     const int j = tid % TPR, d = 4 * j;
-    const int64_t bg = x / R;
-    const int r = (int)(x - bg * R);
+    const int64_t bg = row / R;
+    const int r = (int)(row - bg * R);
     const int b = (int)(bg / c.G), g = (int)(bg - (int64_t)b * c.G);
     float M, L;
     total(bg, r, j, std::integral_constant<int, TPR>{}, M, L);
@@ -865,18 +872,18 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
     const float* po = ws + pl.part_o + (bg * S * R + r) * D + d;
     const float2* ml = reinterpret_cast<const float2*>(ws + pl.part_ml) + bg * S * R + r;
     for (int s0 = group; s0 < S; s0 += 4 * pl.join) {
-      float ms[4];
+      float2 x[4];
       float4 p[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int64_t s = min(s0 + e * pl.join, S - 1);
-        ms[e] = ml[s * R].x;
+        x[e] = ml[s * R];
         p[e] = *reinterpret_cast<const float4*>(po + s * R * D);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (s0 + e * pl.join >= S) break;
-        const float f = ms[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms[e] - M);
+        const float f = x[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[e].x - M) * x[e].y * inv;
         o.x += on_shift(p[e].x, f);
         o.y += on_shift(p[e].y, f);
         o.z += on_shift(p[e].z, f);
@@ -892,14 +899,13 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
           o = make_float4(o.x + p.x, o.y + p.y, o.z + p.z, o.w + p.w);
         }
     }
-    if (x_ >= rows || group != 0) return;
+    if (row_ >= rows || group != 0) return;
     const Row w = row_of(a, b, g, r, R);
     if (M == -INFINITY) o = make_float4(0.f, 0.f, 0.f, 0.f);
-    else o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     store4(out_of<T>(a, b, w) + d, o.x, o.y, o.z, o.w);
     if (j == 0) {
       const float l2 = M == -INFINITY ? -INFINITY : M - Op<T>::kShift + __builtin_amdgcn_logf(L);
-      if (a.weight_out && !pl.by_keys) ((float*)a.ws)[pl.lse2 + x] = l2;
+      if (a.weight_out && !pl.by_keys) ((float*)a.ws)[pl.lse2 + row] = l2;
       if (a.lse) a.lse[((int64_t)b * c.G * a.rep + w.head) * a.n + w.i] = M == -INFINITY ? -INFINITY : l2 * kLn2;
     }
     return;

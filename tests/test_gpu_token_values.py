@@ -57,3 +57,37 @@ def test_values_that_are_not_finite_far_below_the_maximum(dtype, n, C, track):
     assert bool(early[..., 5:7].all())
     tol_lse = 34 * 2.0 ** -24 + 4 * 2.0 ** -24 * math.log(32)
     assert float((lse.double() - math.log(32)).abs().max()) <= tol_lse
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("C", [64, 700, 9000])
+def test_values_near_the_largest(dtype, n, C):
+    """Values up to a quarter of the type's largest: their weighted mean is finite, and so is the result, whatever
+    the sums before the division would come to."""
+    D, N = 64, 3
+    gen = torch.Generator().manual_seed(C + n)
+    k = torch.zeros(1, 1, C, D)
+    k[..., 0] = torch.randint(-40, 41, (C,), generator=gen) / 8.0  # exact in every type, as are the products below
+    v = (0.25 + 0.75 * torch.rand(1, 1, C, D, generator=gen)) * (torch.finfo(dtype).max / 4)
+    v[..., 32:] *= -1
+    k, v = k.to(dtype), v.to(dtype)
+    q = torch.zeros(1, n, N, D)
+    q[..., 0] = torch.tensor([0.0, 1.0, -0.5])
+    at, pos = torch.zeros(1, 1, C, dtype=torch.int32), torch.zeros(1, n, dtype=torch.int32)
+    x = torch.tensor([0.0, 1.0, -0.5]).double()[:, None] * k[0, 0, :, 0].double()
+    p, vd = torch.softmax(x, -1), v[0, 0].double()
+    want = p @ vd
+    # as for ordinary values: scaled scores and log-sum, C + 32 sums and products in fp32, probabilities and the
+    # output rounded to the type
+    u, half = 2.0 ** -24, torch.finfo(dtype).eps / 2
+    rel = 2 * (4 * u * (5 + 8)) + (C + 32) * u
+    tol = (p @ vd.abs()) * (rel + (half if dtype != F32 else u)) + half * want.abs()
+    for track in (False, True):
+        cache = fdb.TokenCache(k.cuda(), v.cuda(), at.cuda(), torch.zeros(1, 1, C).cuda())
+        out, lse = cache.attend(q.to(dtype).cuda(), pos.cuda(), scale=1.0, track=track)
+        assert bool(((out[0].cpu().double() - want).abs() <= tol).all())
+        assert float((lse[0].cpu().double() - torch.logsumexp(x, -1)[:, None]).abs().max()) <= rel + 4 * u * 20
+        if track:
+            total = n * p.sum(0)
+            assert bool(((cache.weight[0, 0].cpu().double() - total).abs() <= total * (2 * rel + (3 * n + 8) * u)).all())
