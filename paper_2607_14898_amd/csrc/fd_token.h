@@ -92,6 +92,7 @@ struct TokenAttendPlan {
   int row_tiles = 1;    // tiles of 32 rows (by_keys) or 128
   int splits = 1;       // parts of the slots
   int scan = 1;         // slots that a workgroup sorts at a time (not by_keys)
+  int fold = 0;         // such ranges between folds of its sums (0: none, not by_keys)
   int weight_parts = 1; // parts of the rows in the pass over the weights
   int row_waves = 1;    // waves that share keys in that pass
   int join = 1;         // groups of threads that share a row's parts when they are joined

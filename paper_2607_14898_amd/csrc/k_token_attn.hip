@@ -26,6 +26,7 @@
 
 #include <stdint.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <type_traits>
 
@@ -72,6 +73,13 @@ template <> struct Op<float> {
     return c;
   }
 };
+
+// Adding n terms one by one in fp32 is off by up to n half steps, and equal terms come close to
+// that: a sum over 2^19 of them in a row was off by 5e-3. So no sum runs on for long: those of
+// single keys or MFMAs end after this many slots (rows) and are added up in turn.
+constexpr int kPartSlots = 16384;       // of a part of attend_keys_kernel (four waves)
+template <typename T> constexpr int kFoldSlots = sizeof(T) == 4 ? 4096 : 16384;  // of attend_rows_kernel
+constexpr int kPartRows = 32768;        // of a part of weights_kernel (32 lanes)
 
 constexpr f32x16 kZero = {};
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -259,6 +267,7 @@ template <typename T, int D, bool EXACT> struct Softmax {
     for (int x0 = 0; x0 < NX; x0 += GX) {
       // (V's fragments are on their way while the exponentials are taken)
       typename O::V ph[GX], pl[GX], vf[GX][D / 32];
+      float add = 0.f;  // (a sum of its own: see kPartSlots)
 #pragma unroll
       for (int y = 0; y < GX; ++y)
 #pragma unroll
@@ -270,13 +279,14 @@ template <typename T, int D, bool EXACT> struct Softmax {
         for (int e = 0; e < 8; ++e) {
           const int x = x0 + y;
           const float p = __builtin_amdgcn_exp2f(fmaf(s[x / 2][8 * (x % 2) + e], c, sub));
-          l += p;
+          add += p;
           // P enters the second MFMA in the cache's type. Where memory bounds the kernel
           // (EXACT) what that rounding loses goes in by a second MFMA; elsewhere its half
           // step per key, as large as the output's own rounding, is kept.
           ph[y][e] = (T)p;
           if constexpr (EXACT && sizeof(T) == 2) pl[y][e] = (T)(p - (float)ph[y][e]);
         }
+      l += add;
       __builtin_amdgcn_s_setprio(2);
 #pragma unroll
       for (int y = 0; y < GX; ++y)
@@ -661,8 +671,43 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
   };
 
   Softmax<T, D, false> sx;
+  // Moves what has been added up to the row's total in the workspace, scaled to the shift that
+  // has been reached since, or (last) takes that total in. Both lanes of a row keep its shift and sum.
+  bool folded = false;
+  auto fold = [&](bool last) __attribute__((always_inline)) {
+    const float L = other_half_sum(sx.l);
+    if (row < R) {
+      const int64_t at = ((int64_t)bg * pl.splits + split) * R + row;
+      float* ml = (float*)a.ws + pl.part_ml + at * 2;
+      float* o = (float*)a.ws + pl.part_o + at * D + 4 * lh;
+      const float f = folded && ml[0] != -INFINITY ? __builtin_amdgcn_exp2f(ml[0] - sx.m) : 0.f;
+      const float l = folded ? ml[1] * f : 0.f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          float4* t = reinterpret_cast<float4*>(o + 32 * d + 2 * r);
+          const float4 x = folded ? *t : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float y[4] = {fmaf(x.x, f, sx.acc[d][r]), fmaf(x.y, f, sx.acc[d][r + 1]),
+                              fmaf(x.z, f, sx.acc[d][r + 2]), fmaf(x.w, f, sx.acc[d][r + 3])};
+          if (!last) *t = make_float4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sx.acc[d][r + e] = last ? y[e] : 0.f;
+        }
+      if (!last) {
+        ml[0] = sx.m;
+        ml[1] = L + l;
+        sx.l = 0.f;
+      } else if (lh == 0) {
+        sx.l += l;
+      }
+    }
+    folded = true;
+  };
   for (int scrub = 0;; scrub = 1) {
     sx.reset();
+    folded = false;
+    int since = 0;  // ranges
     for (c0 = split * kBlock; c0 < c.C; c0 += span) {
       const int c1 = min(c.C, c0 + span);
       auto scanned = [&](int x) {
@@ -685,6 +730,11 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
       seen = scount[0][0] + scount[0][1] + scount[0][2] + scount[0][3];
       m = seen + scount[1][0] + scount[1][1] + scount[1][2] + scount[1][3];
       if (m == 0) continue;
+      if (pl.fold != 0 && since == pl.fold) {
+        fold(false);
+        since = 0;
+      }
+      ++since;
       int at0 = 0, at1 = seen;
       for (int x = 0; x < wave; ++x) {
         at0 += scount[0][x];
@@ -748,6 +798,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
       }
     }
     __syncthreads();
+    if (folded) fold(true);
     if (scrub) {
       sx.m += Op<T>::kDown;
       if (schanged)
@@ -1276,9 +1327,9 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     // whole rounds of what is held, of parts that are long beside what a part costs by
     // itself (about 96 slots' time) but leave two tiles of 32 slots a wave
     int64_t best = INT64_MAX;
-    const int64_t most = clamp(up(c.C, 256), 1, 256);
+    const int64_t least = up(c.C, kPartSlots), most = std::max(clamp(up(c.C, 256), 1, 256), least);
     for (int64_t round = 1; round <= 8; ++round) {
-      const int64_t s = clamp(held * round / wgs, 1, most);
+      const int64_t s = clamp(held * round / wgs, least, most);
       const int64_t cost = up(wgs * s, held) * (up(c.C, s) + 96);
       if (cost < best) {
         best = cost;
@@ -1308,8 +1359,12 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
       }
     }
     p.scan = (int)clamp(blocks / p.splits, 1, kScan / kBlock) * kBlock;
-    const int64_t kw = up(c.C, kind == 2 ? 128 : 256) * BG;
+    const int64_t fold = kind == 2 ? kFoldSlots<float> : kFoldSlots<_Float16>;
+    if (up(up(c.C, kBlock), p.splits) * kBlock > fold) p.fold = (int)std::max<int64_t>(1, fold / p.scan);
+    const int64_t blk = up(c.C, kind == 2 ? 128 : 256), kw = blk * BG;
     p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
+    // (kPartRows, within 2^23 workgroups)
+    p.weight_parts = (int)std::max<int64_t>(p.weight_parts, clamp(up(R, kPartRows), 1, std::max<int64_t>(1, (1 << 23) / blk)));
     p.row_waves = p.weight_parts == 1 && kw * 2 <= held ? 2 : 1;
   }
   int64_t at = 0;
@@ -1320,7 +1375,7 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   };
   const int groups = 256 / (c.D / 4);  // of a row's threads in a workgroup of finish_kernel
   p.join = p.splits >= 32 ? groups : p.splits >= 8 ? 4 : 1;
-  if (p.splits > 1 || (p.by_keys && weights)) {
+  if (p.splits > 1 || p.fold || (p.by_keys && weights)) {
     p.part_o = take(BG * p.splits * R * c.D);
     p.part_ml = take(BG * p.splits * R * 2);
   }
