@@ -5,7 +5,8 @@
 //   (x0, x1) -> m (x0 cos - x1 sin, x0 sin + x1 cos).
 // The angle is taken in 64 bits as a number of turns less the nearest whole one
 // (at position 2^23 an fp32 product would be off by up to half a radian), and only
-// then goes to fp32 for the sine and cosine. All heads of a token share its angles:
+// then goes to fp32 for the sine and cosine; what that rounding took off the angle is
+// turned in afterwards, to first order. All heads of a token share its angles:
 // a workgroup computes each (cos, sin) of its tokens once, into LDS, and then
 // streams the heads' vectors past them, 16 bytes a thread. Both kernels read every
 // element once and write it once, so memory bounds them, and for single tokens the
@@ -34,10 +35,11 @@ __device__ __forceinline__ void fill_angles(const RopeArgs& r, int64_t tok0, int
     const int t = i / r.half, pair = i - t * r.half;
     const int ax = r.axis ? min(max(r.axis[pair], 0), r.axes - 1) : 0;
     const double turns = (double)r.coords[(tok0 + t) * r.axes + ax] * r.freq[pair] * 0.15915494309189533577;
-    const float part = (float)(turns - rint(turns));  // -1/2 .. 1/2
+    const double rest = turns - rint(turns);  // -1/2 .. 1/2
+    const float part = (float)rest, lost = (float)((rest - part) * 6.28318530717958647693);
     float sn, cn;
     sincospif(2.f * part, &sn, &cn);
-    cs[i] = make_float2(cn * r.mag, sn * r.mag * r.sign);
+    cs[i] = make_float2(fmaf(-sn, lost, cn) * r.mag, fmaf(cn, lost, sn) * r.mag * r.sign);
   }
 }
 
