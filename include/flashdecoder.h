@@ -474,7 +474,7 @@ fd_status fd_rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, do
 /* Rotate the head vectors x[token][head][0 .. head_dim) (dtype; strides in
  * elements, any alignment) at coords[token][n_axes] into out, computed in fp32 and
  * rounded once. out may be x with the same strides and must not overlap it
- * otherwise. tokens in [0, 2^31), heads 1 .. 65536, head_dim 1 .. 512. */
+ * otherwise; rows of out that overlap each other are refused. tokens in [0, 2^31), heads 1 .. 65536, head_dim 1 .. 512. */
 fd_status fd_rope_device(const fd_rope* rope, const void* x, int32_t dtype, int64_t tokens, int32_t heads,
                          int32_t head_dim, int64_t x_token_stride, int64_t x_head_stride, const int32_t* coords,
                          void* out, int64_t out_token_stride, int64_t out_head_stride, void* stream);
@@ -523,7 +523,8 @@ fd_status fd_token_slots_device(const int32_t* slot_pos, const float* weight, in
  * both [batch][n][groups][head_dim] of the cache's dtype by strides (host arrays:
  * batch, token, group; whole 16 bytes, rows 16-byte aligned), pos, and weight 0.
  * coords NULL: pos is the one coordinate. Tokens with pos < 0 or a slot outside
- * [0, capacity) are left out. The slots of one (request, group) must differ, as
+ * [0, capacity) are left out. A cache whose rows overlap is refused; k and v lie outside
+ * it. The slots of one (request, group) must differ, as
  * fd_token_slots_device's do: where two tokens name one slot, it is left with
  * parts of both. */
 fd_status fd_token_append_device(const fd_token_cache* cache, const fd_rope* rope, const void* k,
@@ -547,7 +548,8 @@ fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, 
  * probability. A decoder's frame mask is causal = 1 with the frame index as every token's
  * position.
  *   q, out      [batch][n][heads][head_dim] of the cache's dtype by strides (host arrays:
- *               batch, token, head; whole 16 bytes), rows 16-byte aligned, no overlap
+ *               batch, token, head; whole 16 bytes), rows 16-byte aligned, no overlap of
+ *               q and out (rows of out that overlap each other are refused)
  *   lse         [batch][heads][n] fp32, or NULL
  *   weight_out  [batch][groups][capacity], may be the cache's weight, or NULL: not
  *               computed

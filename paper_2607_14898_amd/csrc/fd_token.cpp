@@ -2,6 +2,7 @@
 // launcher each.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 
@@ -49,6 +50,38 @@ bool strides_ok(const int64_t* s, std::initializer_list<int64_t> extents, int he
     ++s;
   }
   return true;
+}
+
+// Whether two rows of `width` elements at these strides (at least width where the extent is above
+// one) share an element. Layouts that nest, as views of one tensor do, are seen at once; for
+// others the distances along all axes but the longest are gone through, and the nearest
+// steps of that one back.
+bool rows_overlap(std::initializer_list<int64_t> strides, std::initializer_list<int64_t> extents, int64_t width) {
+  struct Axis { int64_t stride, extent; } ax[3];
+  int n = 0;
+  for (auto s = strides.begin(), e = extents.begin(); s != strides.end(); ++s, ++e)
+    if (*e > 1) ax[n++] = {*s, *e};
+  std::sort(ax, ax + n, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  __int128 span = width;
+  bool nested = true;
+  for (int i = 0; i < n; ++i) {
+    nested = nested && ax[i].stride >= span;
+    span += (__int128)(ax[i].extent - 1) * ax[i].stride;
+  }
+  if (nested) return false;
+  std::sort(ax, ax + n, [](const Axis& a, const Axis& b) { return a.extent > b.extent; });
+  const Axis b = n > 1 ? ax[1] : Axis{0, 1}, c = n > 2 ? ax[2] : Axis{0, 1};
+  for (int64_t i = 0; i < b.extent; ++i)
+    for (int64_t j = 1 - c.extent; j < c.extent; ++j) {
+      const __int128 off = (__int128)i * b.stride + (__int128)j * c.stride;
+      const __int128 k = off / ax[0].stride;  // and its neighbours
+      for (int d = -1; d <= 1; ++d) {
+        const __int128 x = off - (k + d) * ax[0].stride;
+        const bool far = k + d >= ax[0].extent || k + d <= -(__int128)ax[0].extent;
+        if (!far && x < width && -x < width && (i || j || k + d)) return true;
+      }
+    }
+  return false;
 }
 
 fd_status check_cache(const fd_token_cache* c, fd::TokenCacheArgs* a) {
@@ -147,7 +180,8 @@ fd_status fd_rope_device(const fd_rope* rope, const void* x, int32_t dtype, int6
   w.o_head = out_head_stride;
   for (int64_t s : {x_token_stride, x_head_stride, out_token_stride, out_head_stride})
     if (s < 0 || s >= (int64_t)1 << 48) return fail(FD_ERR_INVALID_ARGUMENT, "strides must be in [0, 2^48)");
-  if ((tokens > 1 && out_token_stride < head_dim) || (heads > 1 && out_head_stride < head_dim))
+  if ((tokens > 1 && out_token_stride < head_dim) || (heads > 1 && out_head_stride < head_dim) ||
+      rows_overlap({out_token_stride, out_head_stride}, {tokens, heads}, head_dim))
     return fail(FD_ERR_INVALID_ARGUMENT, "rows of out overlap");
   if (x == out && ((tokens > 1 && x_token_stride != out_token_stride) || (heads > 1 && x_head_stride != out_head_stride)))
     return fail(FD_ERR_INVALID_ARGUMENT, "in place needs the same strides for x and out");
@@ -219,6 +253,9 @@ fd_status fd_token_append_device(const fd_token_cache* cache, const fd_rope* rop
   if (n < 0 || (int64_t)c.B * n > 0x7FFFFFFF)
     return fail(FD_ERR_INVALID_ARGUMENT, "n >= 0 and batch x n below 2^31 required");
   if (n == 0) return FD_OK;
+  for (const int64_t* x : {c.ks, c.vs})
+    if (rows_overlap({x[0], x[1], x[2]}, {c.B, c.G, c.C}, c.D))
+      return fail(FD_ERR_INVALID_ARGUMENT, "rows of the cache overlap");
   if (!k || !v || !k_stride || !v_stride || !pos || !slots) return fail(FD_ERR_INVALID_ARGUMENT, "NULL pointer");
   if (r.half > 0 && !coords && r.axes != 1)
     return fail(FD_ERR_INVALID_ARGUMENT, "coords may be NULL only for one axis (then pos turns the keys)");
@@ -295,6 +332,8 @@ fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, con
       return fail(FD_ERR_INVALID_ARGUMENT, "q and out must be 16-byte aligned, pos 4-byte aligned");
     if (!strides_ok(q_stride, extents, c.D, es) || !strides_ok(out_stride, extents, c.D, es))
       return fail(FD_ERR_INVALID_ARGUMENT, "strides of q and out must be at least head_dim and whole 16 bytes");
+    if (rows_overlap({out_stride[0], out_stride[1], out_stride[2]}, {c.B, n, heads}, c.D))
+      return fail(FD_ERR_INVALID_ARGUMENT, "rows of out overlap");
     plan = fd::token_attend_plan(c, n, rep, kind, weight_out != nullptr);
     const int64_t need = plan.bytes;
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < (size_t)need))
