@@ -310,7 +310,9 @@ fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, con
   fd_status st = check_cache(cache, &c);
   if (st != FD_OK) return st;
   if ((st = check_attend(c, heads, n)) != FD_OK) return st;
-  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(FD_ERR_INVALID_ARGUMENT, "scale must be finite and > 0");
+  // (the kernels take powers of two: scale log2 e, which need not be finite where scale is)
+  if (!std::isfinite(scale * 1.44269504f) || !(scale > 0.f))
+    return fail(FD_ERR_INVALID_ARGUMENT, "scale must be > 0, and scale / ln 2 finite in fp32");
   if (!std::isfinite(decay)) return fail(FD_ERR_INVALID_ARGUMENT, "decay must be finite");
   if ((uintptr_t)weight_out % 4 || (uintptr_t)lse % 4)
     return fail(FD_ERR_INVALID_ARGUMENT, "lse and weight_out must be 4-byte aligned");

@@ -71,3 +71,13 @@ def test_rows_of_attention_and_cache_that_overlap():
         st = _attend_call(lib, c, qs=(4096, 64, 1024), os_=(s[0], s[2], s[1]), heads=G, n=C, ws=None)
         assert _says(lib, st, "overlap") == want, (B, G, C, s)
     assert min(found.values()) > 50
+
+
+def test_scales_beyond_fp32():
+    """The kernels work in powers of two: a scale whose scale / ln 2 is no fp32 number is refused."""
+    lib = _lib()
+    most = float(np.finfo(np.float32).max) * math.log(2)
+    for scale in (most * 1.0001, 3e38, float(np.finfo(np.float32).max)):
+        assert _says(lib, _attend_call(lib, scale=scale), "scale"), scale
+    for scale in (most * 0.9999, 1e30, 1e-38):
+        assert _says(lib, _attend_call(lib, scale=scale, ws=None), "workspace"), scale
