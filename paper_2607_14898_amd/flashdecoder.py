@@ -516,6 +516,15 @@ def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> Non
     raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
 
 
+def _no_grad(hint: str, *tensors) -> None:
+    """ValueError if autograd would record a call on these tensors, which it cannot see."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                raise ValueError(f"an input requires grad, which this call would lose: {hint}")
+
+
 _codes: Dict = {}  # torch dtype -> FD_DTYPE_*
 
 
@@ -606,8 +615,11 @@ class Rope:
 
     def __call__(self, x, coords, out=None, stream=None):
         """Rotate x [tokens, heads, head_dim] (fp32, bf16 or fp16; strided) at coords
-        [tokens] or [tokens, n_axes] (int32); out may be x."""
+        [tokens] or [tokens, n_axes] (int32); out may be x. Autograd does not see it: the
+        gradient of x is ``inverted()`` of out's, and an x that requires grad is refused
+        while gradients are recorded."""
         import torch
+        _no_grad("rotate under torch.no_grad() and turn its gradient back with inverted()", x, out)
         tokens, heads, dim = x.shape
         dt, dev = _dtype_code(x, "x"), self.freq.device
         _need(x, "x", x.dtype, x.shape, dev, strided=True)
@@ -648,7 +660,12 @@ class TokenCache:
     capacity, head_dim] (strided), pos int32 and weight fp32 [batch, groups, capacity].
 
     A step of a stream: ``insert`` the new tokens' keys and values (the least attended
-    tokens make room), then ``attend`` with their queries, which adds to the weights."""
+    tokens make room), then ``attend`` with their queries, which adds to the weights.
+
+    For serving: no gradient passes, and tensors that require one are refused while
+    gradients are recorded."""
+
+    _SERVING = "call it under torch.no_grad() or detach it"
 
     def __init__(self, k, v, pos, weight):
         import torch
@@ -690,6 +707,7 @@ class TokenCache:
         """Write k (rotated by rope at coords [batch, n, n_axes], default pos) and v
         [batch, n, groups, head_dim] into their slots (fd_token_append_device)."""
         import torch
+        _no_grad(self._SERVING, k, v, self.k, self.v)
         dev, n = self.pos.device, pos.shape[-1]
         shape = (self.batch, n, self.groups, self.head_dim)
         _need(k, "k", self.k.dtype, shape, dev, strided=True)
@@ -719,6 +737,7 @@ class TokenCache:
         [batch, heads, n]). With track the slots' weights become decay x weight + what
         they received, in place or in weight_out."""
         import torch
+        _no_grad(self._SERVING, q, self.k, self.v, out)
         B, n, heads, D = q.shape
         dev = self.pos.device
         _need(q, "q", self.k.dtype, (self.batch, n, heads, self.head_dim), dev, strided=True)
