@@ -1321,8 +1321,14 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
   p.by_keys = R <= 64;
   p.row_tiles = (int)up(R, p.by_keys ? 32 : 128);
   const int64_t wgs = BG * p.row_tiles;
-  // workgroups that the chip holds at once (by registers and LDS)
-  const int64_t held = 256 * (c.D < 128 ? 3 : kind == 2 ? 1 : 2);
+  // workgroups that the chip holds at once, by the kernels' registers (LDS allows as many):
+  // attend_keys_kernel, and weights_kernel for one and two waves that share keys. (One token, 8
+  // groups x 4 heads, 65536 slots, 64 dims, fp32: 67 us by the two a CU that fit, 84 by three. Of
+  // 32 dims four fit, but three are as fast or faster: 131072 slots, bf16, 37 us against 38.)
+  const int fp32 = kind == 2;
+  const int64_t held = 256 * (c.D == 128 ? 2 - fp32 : c.D == 64 ? 3 - fp32 : 3);
+  const int64_t held_w1 = 256 * (c.D == 128 ? 2 : 3 + (fp32 && c.D == 32));
+  const int64_t held_w2 = 256 * (fp32 ? (c.D == 128 ? 2 : c.D == 64 ? 3 : 4) : c.D == 32 ? 3 : 2);
   if (p.by_keys) {
     // whole rounds of what is held, of parts that are long beside what a part costs by
     // itself (about 96 slots' time) but leave two tiles of 32 slots a wave
@@ -1362,10 +1368,10 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     const int64_t fold = kind == 2 ? kFoldSlots<float> : kFoldSlots<_Float16>;
     if (up(up(c.C, kBlock), p.splits) * kBlock > fold) p.fold = (int)std::max<int64_t>(1, fold / p.scan);
     const int64_t blk = up(c.C, kind == 2 ? 128 : 256), kw = blk * BG;
-    p.weight_parts = (int)clamp(held / kw, 1, clamp(R / 256, 1, 64));
+    p.weight_parts = (int)clamp(held_w1 / kw, 1, clamp(R / 256, 1, 64));
     // (kPartRows, within 2^23 workgroups)
     p.weight_parts = (int)std::max<int64_t>(p.weight_parts, clamp(up(R, kPartRows), 1, std::max<int64_t>(1, (1 << 23) / blk)));
-    p.row_waves = p.weight_parts == 1 && kw * 2 <= held ? 2 : 1;
+    p.row_waves = p.weight_parts == 1 && kw * 2 <= held_w2 ? 2 : 1;
   }
   int64_t at = 0;
   auto take = [&](int64_t floats) {

@@ -53,3 +53,12 @@ def test_many_rows_part_their_weights():
     R = heads * n
     got = workspace(1, 1, C, 32, heads, n, "bf16") - workspace(1, 1, C, 32, heads, n, "bf16", weights=0)
     assert got >= up64(R) + up64(R // 32768 * C)
+
+
+@pytest.mark.parametrize("dtype,D,held", [("f32", 64, 512), ("bf16", 64, 768), ("f16", 128, 512), ("f32", 128, 256)])
+def test_single_tokens_fill_whole_rounds(dtype, D, held):
+    """Parts of few rows make whole rounds of the workgroups that fit on 256 CUs at once."""
+    G, C = 8, 65536
+    got = workspace(1, G, C, D, 4 * G, 1, dtype, weights=0)
+    fits = [s for s in range(1, 257) if parts_floats(G, s, 4, D) == got]
+    assert len(fits) == 1 and fits[0] * G % held == 0
