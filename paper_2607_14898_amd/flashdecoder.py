@@ -704,7 +704,8 @@ class TokenCache:
         return slots
 
     def append(self, k, v, pos, slots, rope: Optional[Rope] = None, coords=None, stream=None) -> None:
-        """Write k (rotated by rope at coords [batch, n, n_axes], default pos) and v
+        """Write k (rotated by rope at coords [batch, n, n_axes] or, for one axis, [batch, n];
+        default pos) and v
         [batch, n, groups, head_dim] into their slots (fd_token_append_device)."""
         import torch
         _no_grad(self._SERVING, k, v, self.k, self.v)
@@ -715,7 +716,9 @@ class TokenCache:
         _need(pos, "pos", torch.int32, (self.batch, n), dev)
         _need(slots, "slots", torch.int32, (self.batch, self.groups, n), dev)
         if coords is not None:
-            _need(coords, "coords", torch.int32, (self.batch, n, rope.n_axes if rope else 1), dev)
+            axes = rope.n_axes if rope else 1
+            _need(coords, "coords", torch.int32, (self.batch, n, axes) if coords.dim() == 3 or axes > 1 else
+                  (self.batch, n), dev)
         if rope is not None and rope.freq.device != dev:
             raise ValueError(f"rope on {rope.freq.device} for a cache on {dev}")
         I3 = ctypes.c_int64 * 3

@@ -48,3 +48,20 @@ def test_inputs_that_require_grad():
     w = torch.randn_like(x[0])
     (Turn.apply(leaf[0]) * w).sum().backward()
     assert torch.equal(leaf.grad[0], rope.inverted()(w, pos[0]))
+
+
+def test_coordinates_of_one_axis():
+    """append takes them as [batch, n] or [batch, n, 1], as a rotation does; other shapes are refused."""
+    cache, rope, x, pos = _setup()
+    slots, coords = cache.choose(pos), pos * 7 + 2
+    cache.append(x, x, pos, slots, rope, coords[..., None].contiguous())
+    want = cache.k.clone()
+    cache.k.zero_()
+    cache.append(x, x, pos, slots, rope, coords)
+    assert torch.equal(cache.k, want) and bool(want.any())
+    for bad in (coords[0], coords[:, :2].contiguous(), coords[..., None].expand(1, 3, 2).contiguous(), coords.long()):
+        with pytest.raises(ValueError):
+            cache.append(x, x, pos, slots, rope, bad)
+    three = fdb.Rope(rope.freq, torch.zeros(32, dtype=torch.int32, device="cuda"), 3)
+    with pytest.raises(ValueError):
+        cache.append(x, x, pos, slots, three, coords)
