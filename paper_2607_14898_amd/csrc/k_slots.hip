@@ -18,6 +18,8 @@
 // where one workgroup's instructions and barriers are the limit and not memory.
 // Integer counts only: the result does not depend on the order of the atomics.
 // One new token (serving) is a plain minimum of (class, weight, slot): 2.7 us at 1024 slots.
+// The one workgroup of a pair reads what a CU can (8 bytes a slot at 37 GB/s): 28 us at 131072
+// slots, 107 at 524288; there chunks are faster while they find idle CUs (chunks_of).
 #include "fd_token.h"
 
 #include <type_traits>
@@ -334,7 +336,9 @@ __global__ __launch_bounds__(kThreads) void slots_kernel(TokenSlots a) {
 }
 
 // One new token: the least (class, weight, slot). U loads of each array are under way (a
-// few thousand slots are one or two a thread: eight would load the last one over and over).
+// few thousand slots are one to four a thread, and eight would load the last one over and
+// over: 1024 slots 2.8 us against 4.1, 4096 3.0 to 3.6 against 3.8 to 4.3, 8192 alike; from
+// there on eight are faster, 17.7 us against 28.5 for 128 pairs of 65536).
 template <int U>
 __global__ __launch_bounds__(kThreads) void slot_least_kernel(TokenSlots a) {
   __shared__ uint64_t part[kWaves];
@@ -383,20 +387,25 @@ hipError_t choose(const TokenSlots& a, unsigned blocks, int keys, hipStream_t s)
   return hipGetLastError();
 }
 
-// Chunks of a first launch, or 0: one launch.
-int64_t chunks_of(int capacity, int n) {
+// Chunks of a first launch, or 0: one launch. For one token that is a plain minimum, 3.5 us a
+// chunk of its pair, while chunks cost 15 us a round of 256 workgroups and 10 to join (measured: 8
+// pairs of 131072 slots 24 us against 28, of 2^20 42 against 224; 32 of 262144 43 against 59; but 64
+// pairs of 131072 43 against 32).
+int64_t chunks_of(int64_t pairs, int capacity, int n) {
   const int64_t chunks = ((int64_t)capacity + kChunk - 1) / kChunk;
+  if (n == 1) return 3.5 * (double)chunks > 15.0 * (double)((pairs * chunks + 255) / 256) + 10.0 ? chunks : 0;
   return capacity > kChunk && n > 1 && chunks * n <= capacity / 2 ? chunks : 0;
 }
 }  // namespace
 
 int64_t token_slots_workspace(int batch, int groups, int capacity, int n) {
-  return (int64_t)batch * groups * chunks_of(capacity, n) * n * 4;
+  const int64_t pairs = (int64_t)batch * groups;
+  return pairs * chunks_of(pairs, capacity, n) * n * 4;
 }
 
 hipError_t token_slots(TokenSlots a, hipStream_t s) {
   const dim3 grid((unsigned)(a.B * a.G));
-  const int64_t chunks = chunks_of(a.C, a.n);
+  const int64_t chunks = chunks_of((int64_t)a.B * a.G, a.C, a.n);
   if (chunks > 0) {
     TokenSlots f = a;
     f.chunks = a.chunks = (int)chunks;
@@ -407,7 +416,7 @@ hipError_t token_slots(TokenSlots a, hipStream_t s) {
     return choose(a, (unsigned)(a.B * a.G), (int)chunks * a.n, s);
   }
   if (a.n > 1) return choose(a, (unsigned)(a.B * a.G), a.C, s);
-  if (a.C <= 2 * kThreads) hipLaunchKernelGGL(slot_least_kernel<1>, grid, dim3(kThreads), 0, s, a);
+  if (a.C <= 4 * kThreads) hipLaunchKernelGGL(slot_least_kernel<1>, grid, dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL(slot_least_kernel<8>, grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }

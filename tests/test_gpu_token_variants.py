@@ -244,3 +244,29 @@ def test_choice_among_more_candidates_than_registers_hold(C, n, ties):
             want = np.full(n, -1)
             want[valid] = np.sort(order[: len(valid)])
             assert np.array_equal(got[b, g], want), (b, g)
+
+
+@pytest.mark.parametrize("B,G,C", [(1, 1, 131072), (2, 3, 150001), (1, 2, 1 << 20), (8, 4, 131100), (33, 2, 131100), (2, 2, 3000),
+                                   (2, 2, 4097)])
+def test_one_token_among_many_slots(B, G, C):
+    """In one launch and in chunks, with ties, empty slots and padding."""
+    r = np.random.default_rng(C)
+    at = r.integers(0, 2 * C, (B, G, C)).astype(np.int32)
+    weight = r.integers(1, 50, (B, G, C)).astype(np.float32)
+    weight[0, 0, C - 1] = 0.0
+    if G > 1:
+        at[:, 1, C - 2] = -1
+        weight[0, 1, C // 2] = np.nan
+    pos = np.full((B, 1), 2 * C, np.int32)
+    pos[B // 2 if B > 1 else 1:] = -1
+    for first, recent in ((3, C // 2), (0, 0), (2 * C, 0)):
+        got = _slots(at, weight, pos, first, recent)
+        for b in range(B):
+            for g in range(G):
+                if pos[b, 0] < 0:
+                    assert got[b, g, 0] == -1
+                    continue
+                p, w = at[b, g].astype(np.int64), weight[b, g].astype(np.float64)
+                kind = np.where(p < 0, 0, np.where(p < first, 3, np.where(p > 2 * C - recent, 2, 1)))
+                w = np.where(kind > 0, np.where(np.isnan(w), -np.inf, w), 0.0)
+                assert got[b, g, 0] == np.lexsort((np.arange(C), w, kind))[0], (b, g, first)

@@ -62,3 +62,15 @@ def test_single_tokens_fill_whole_rounds(dtype, D, held):
     got = workspace(1, G, C, D, 4 * G, 1, dtype, weights=0)
     fits = [s for s in range(1, 257) if parts_floats(G, s, 4, D) == got]
     assert len(fits) == 1 and fits[0] * G % held == 0
+
+
+@pytest.mark.parametrize("B,G,C,n,chunks", [(1, 8, 131072, 1, 8), (1, 1, 1 << 24, 1, 1024), (4, 8, 262144, 1, 16),
+                                            (1, 1, 100000, 1, 0), (8, 8, 131072, 1, 0), (16, 8, 262144, 1, 0),
+                                            (1, 1, 131072, 0, 0)])
+def test_one_token_among_many_slots(B, G, C, n, chunks):
+    """Chunks of 16384 slots, four bytes each, where one workgroup a pair would leave the chip idle for long."""
+    if not os.path.exists(fdb.LIB_PATH):
+        pytest.skip("libflashdecoder.so not built")
+    size = ctypes.c_size_t()
+    assert fdb.load_library().fd_token_slots_workspace(B, G, C, n, ctypes.byref(size)) == fdb.FD_OK
+    assert size.value == 4 * B * G * chunks
