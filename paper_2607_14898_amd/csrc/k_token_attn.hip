@@ -860,12 +860,14 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows
 }
 
 // What is left when the parts are done: workgroups below row_blocks join the parts of
-// rows (D / 4 threads each), the others add up what rows gave kFinishSlots slots each,
+// rows (D / 4 threads each), the others add up what rows gave 256 NS slots each,
 // from the scores that attend_keys_kernel kept (4 bytes a row and slot, beside 4 D of a
 // 16-bit key and value). Each of those works out its rows' log-sums from the parts by
-// itself, 16 threads a row (64 for many parts). Parts are read side by side throughout: a chain of dependent
+// itself, 16 threads a row (64 for 256 parts: a call of 4 rows 19.7 us against 20.4, of 28 rows
+// 35.5 against 29.7). Parts are read side by side throughout: a chain of dependent
 // loads per part cost 0.7 us each.
-// Four slots a thread once that still leaves two workgroups a CU.
+// Four slots a thread once that still leaves two workgroups a CU (2^19 slots in all; a whole call
+// of one token, 8 x 8 groups of 2048 slots 14.9 us with one and 15.8 with four, of 8192 34.8 and 33.4).
 constexpr int kFinishRows = 64;
 template <typename T, int D, int NS>
 __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl,
@@ -977,19 +979,15 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
   for (int r0 = 0; r0 < R; r0 += kFinishRows) {
     const int m = min(kFinishRows, R - r0);
     __syncthreads();
-    auto sums = [&](auto width) {
-      constexpr int W = decltype(width)::value, RG = 256 / W;
-      for (int q = tid / W; q < (m + RG - 1) / RG * RG; q += RG) {
-        float M, L;
-        total(bg, r0 + min(q, m - 1), tid % W, width, M, L);
-        if (tid % W == 0 && q < m) {
-          s_l2[q] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
-          s_lim[q] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + q, R).lim;
-        }
+    constexpr int W = 16, RG = 256 / W;
+    for (int q = tid / W; q < (m + RG - 1) / RG * RG; q += RG) {
+      float M, L;
+      total(bg, r0 + min(q, m - 1), tid % W, std::integral_constant<int, W>{}, M, L);
+      if (tid % W == 0 && q < m) {
+        s_l2[q] = M - Op<T>::kShift + __builtin_amdgcn_logf(L);
+        s_lim[q] = M == -INFINITY ? 0u : row_of(a, b, g, r0 + q, R).lim;
       }
-    };
-    if (S > 64) sums(std::integral_constant<int, 64>{});
-    else sums(std::integral_constant<int, 16>{});
+    }
     __syncthreads();
     const float* sc[NS];
 #pragma unroll
@@ -1379,7 +1377,9 @@ TokenAttendPlan token_attend_plan(const TokenCacheArgs& c, int n, int rep, int k
     at += up(floats, 64) * 64;
     return o;
   };
-  const int groups = 256 / (c.D / 4);  // of a row's threads in a workgroup of finish_kernel
+  // Groups of a row's threads in a workgroup of finish_kernel (4 rows, 64 dims: 64 parts by one
+  // group 32 us in all, by four 16, by sixteen 12; 256 parts 100, 36 and 20).
+  const int groups = 256 / (c.D / 4);
   p.join = p.splits >= 32 ? groups : p.splits >= 8 ? 4 : 1;
   if (p.splits > 1 || p.fold || (p.by_keys && weights)) {
     p.part_o = take(BG * p.splits * R * c.D);
