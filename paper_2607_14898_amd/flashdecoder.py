@@ -525,6 +525,13 @@ def _no_grad(hint: str, *tensors) -> None:
                 raise ValueError(f"an input requires grad, which this call would lose: {hint}")
 
 
+def _int32(**values) -> None:
+    """ValueError for numbers that the C interface's int32 would silently cut."""
+    for name, x in values.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{name} {x} is no 32-bit integer")
+
+
 _codes: Dict = {}  # torch dtype -> FD_DTYPE_*
 
 
@@ -577,7 +584,8 @@ def fd_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "no
                         trained_length: float = 0.0, fast_turns: float = 32.0, slow_turns: float = 1.0):
     """(frequencies float64 numpy [rot_dim / 2], magnitude) of a rotary embedding;
     scaling "none", "linear", "base" or "bands"."""
-    freq = np.empty(max(rot_dim, 0) // 2, np.float64)
+    _int32(rot_dim=rot_dim)
+    freq = np.empty(min(max(rot_dim, 0), 512) // 2, np.float64)  # (of more none is written)
     mag = ctypes.c_float()
     if scaling not in _ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(_ROPE_SCALINGS)}")
@@ -597,6 +605,7 @@ class Rope:
             raise ValueError(f"layout must be one of {sorted(_ROPE_LAYOUTS)}")
         if not isinstance(freq, torch.Tensor):
             freq = torch.from_numpy(np.ascontiguousarray(freq, np.float64)).to(device)
+        _int32(n_axes=n_axes)
         _need(freq, "freq", torch.float64, freq.shape if freq.dim() == 1 else (freq.numel(),))
         if axis is not None:
             if not isinstance(axis, torch.Tensor):
@@ -639,6 +648,7 @@ def fd_token_slots_device(slot_pos, weight, pos, slots, keep_first: int = 0, kee
     """Slots (int32 [batch, groups, n]) for n new tokens at pos (int32 [batch, n], < 0:
     padding) of a cache with positions slot_pos and weights [batch, groups, capacity]."""
     import torch
+    _int32(keep_first=keep_first, keep_recent=keep_recent)
     B, G, C = slot_pos.shape
     n, dev = pos.shape[-1], slot_pos.device
     _need(slot_pos, "slot_pos", torch.int32, slot_pos.shape)

@@ -81,3 +81,20 @@ def test_scales_beyond_fp32():
         assert _says(lib, _attend_call(lib, scale=scale), "scale"), scale
     for scale in (most * 0.9999, 1e30, 1e-38):
         assert _says(lib, _attend_call(lib, scale=scale, ws=None), "workspace"), scale
+
+
+def test_numbers_beyond_int32():
+    """A count of 2^32 is not taken for 0, nor 2^32 + 64 for 64."""
+    import torch
+    _lib()
+    z = torch.zeros(1, 1, 4, dtype=torch.int32)
+    for kw in (dict(keep_recent=2 ** 32), dict(keep_first=2 ** 32 + 4), dict(keep_recent=2 ** 31)):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            fdb.fd_token_slots_device(z, torch.zeros(1, 1, 4), z[0], z, **kw)
+    for rot_dim in (2 ** 32 + 64, -2 ** 32 + 64):
+        with pytest.raises(ValueError, match="rot_dim"):
+            fdb.fd_rope_frequencies(rot_dim)
+    with pytest.raises(fdb.FlashDecoderError):
+        fdb.fd_rope_frequencies(2 ** 31 - 2)
+    with pytest.raises(ValueError, match="n_axes"):
+        fdb.Rope(torch.ones(32, dtype=torch.float64), n_axes=2 ** 32 + 1)
