@@ -516,20 +516,21 @@ def _need(t, name: str, dtype, shape, device=None, strided: bool = False) -> Non
     raise ValueError(f"{name} must be contiguous" + (" in its last dimension" if strided else ""))
 
 
-def _no_grad(hint: str, *tensors) -> None:
-    """ValueError if autograd would record a call on these tensors, which it cannot see."""
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            import torch
-            if torch.is_grad_enabled():
-                raise ValueError(f"an input requires grad, which this call would lose: {hint}")
+def _no_grad(hint: str) -> None:
+    """For a call with a tensor that requires grad: ValueError if autograd would record it,
+    which cannot see it."""
+    import torch
+    if torch.is_grad_enabled():
+        raise ValueError(f"an input requires grad, which this call would lose: {hint}")
 
 
-def _int32(**values) -> None:
-    """ValueError for numbers that the C interface's int32 would silently cut."""
-    for name, x in values.items():
-        if not -2 ** 31 <= x < 2 ** 31:
-            raise ValueError(f"{name} {x} is no 32-bit integer")
+_INT32_MAX = 2 ** 31 - 1
+
+
+def _int32(name: str, x: int) -> None:
+    """ValueError for a number that the C interface's int32 would silently cut."""
+    if not -_INT32_MAX - 1 <= x <= _INT32_MAX:
+        raise ValueError(f"{name} {x} is no 32-bit integer")
 
 
 _codes: Dict = {}  # torch dtype -> FD_DTYPE_*
@@ -584,7 +585,7 @@ def fd_rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "no
                         trained_length: float = 0.0, fast_turns: float = 32.0, slow_turns: float = 1.0):
     """(frequencies float64 numpy [rot_dim / 2], magnitude) of a rotary embedding;
     scaling "none", "linear", "base" or "bands"."""
-    _int32(rot_dim=rot_dim)
+    _int32("rot_dim", rot_dim)
     freq = np.empty(min(max(rot_dim, 0), 512) // 2, np.float64)  # (of more none is written)
     mag = ctypes.c_float()
     if scaling not in _ROPE_SCALINGS:
@@ -605,7 +606,7 @@ class Rope:
             raise ValueError(f"layout must be one of {sorted(_ROPE_LAYOUTS)}")
         if not isinstance(freq, torch.Tensor):
             freq = torch.from_numpy(np.ascontiguousarray(freq, np.float64)).to(device)
-        _int32(n_axes=n_axes)
+        _int32("n_axes", n_axes)
         _need(freq, "freq", torch.float64, freq.shape if freq.dim() == 1 else (freq.numel(),))
         if axis is not None:
             if not isinstance(axis, torch.Tensor):
@@ -628,7 +629,8 @@ class Rope:
         gradient of x is ``inverted()`` of out's, and an x that requires grad is refused
         while gradients are recorded."""
         import torch
-        _no_grad("rotate under torch.no_grad() and turn its gradient back with inverted()", x, out)
+        if x.requires_grad or (out is not None and out.requires_grad):
+            _no_grad("rotate under torch.no_grad() and turn its gradient back with inverted()")
         tokens, heads, dim = x.shape
         dt, dev = _dtype_code(x, "x"), self.freq.device
         _need(x, "x", x.dtype, x.shape, dev, strided=True)
@@ -648,7 +650,8 @@ def fd_token_slots_device(slot_pos, weight, pos, slots, keep_first: int = 0, kee
     """Slots (int32 [batch, groups, n]) for n new tokens at pos (int32 [batch, n], < 0:
     padding) of a cache with positions slot_pos and weights [batch, groups, capacity]."""
     import torch
-    _int32(keep_first=keep_first, keep_recent=keep_recent)
+    if abs(keep_first) > _INT32_MAX or abs(keep_recent) > _INT32_MAX:  # (ctypes cuts them in silence)
+        raise ValueError(f"keep_first {keep_first} and keep_recent {keep_recent} must be in [0, 2^31)")
     B, G, C = slot_pos.shape
     n, dev = pos.shape[-1], slot_pos.device
     _need(slot_pos, "slot_pos", torch.int32, slot_pos.shape)
@@ -718,7 +721,8 @@ class TokenCache:
         default pos) and v
         [batch, n, groups, head_dim] into their slots (fd_token_append_device)."""
         import torch
-        _no_grad(self._SERVING, k, v, self.k, self.v)
+        if k.requires_grad or v.requires_grad or self.k.requires_grad or self.v.requires_grad:
+            _no_grad(self._SERVING)
         dev, n = self.pos.device, pos.shape[-1]
         shape = (self.batch, n, self.groups, self.head_dim)
         _need(k, "k", self.k.dtype, shape, dev, strided=True)
@@ -750,7 +754,9 @@ class TokenCache:
         [batch, heads, n]). With track the slots' weights become decay x weight + what
         they received, in place or in weight_out."""
         import torch
-        _no_grad(self._SERVING, q, self.k, self.v, out)
+        if (q.requires_grad or self.k.requires_grad or self.v.requires_grad
+                or (out is not None and out.requires_grad)):
+            _no_grad(self._SERVING)
         B, n, heads, D = q.shape
         dev = self.pos.device
         _need(q, "q", self.k.dtype, (self.batch, n, heads, self.head_dim), dev, strided=True)
