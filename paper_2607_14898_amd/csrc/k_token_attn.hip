@@ -935,12 +935,18 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (s0 + e * pl.join >= S) break;
-        const float f = x[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[e].x - M) * x[e].y * inv;
-        o.x += on_shift(p[e].x, f);
-        o.y += on_shift(p[e].y, f);
-        o.z += on_shift(p[e].z, f);
-        o.w += on_shift(p[e].w, f);
+        const float f = s0 + e * pl.join >= S || x[e].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[e].x - M) * x[e].y * inv;
+        if (f != 0.f) {
+          o.x = fmaf(f, p[e].x, o.x);
+          o.y = fmaf(f, p[e].y, o.y);
+          o.z = fmaf(f, p[e].z, o.z);
+          o.w = fmaf(f, p[e].w, o.w);
+        } else {
+          o.x += on_shift(p[e].x, 0.f);
+          o.y += on_shift(p[e].y, 0.f);
+          o.z += on_shift(p[e].z, 0.f);
+          o.w += on_shift(p[e].w, 0.f);
+        }
       }
     }
     if (pl.join > 1) {
