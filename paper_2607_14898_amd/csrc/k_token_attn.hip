@@ -281,8 +281,11 @@ template <typename T, int D, bool EXACT> struct Softmax {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[x / 2][8 * (x % 2) + e], c, sub));
           add += p;
           // P enters the second MFMA in the cache's type. Where memory bounds the kernel
-          // (EXACT) what that rounding loses goes in by a second MFMA; elsewhere its half
-          // step per key, as large as the output's own rounding, is kept.
+          // (EXACT) what that rounding loses goes in by a second MFMA; elsewhere, where it would
+          // be half as many MFMAs again, its half step per key, as large as the output's own
+          // rounding, is kept (the sum that it is divided by is of unrounded ones). Error against
+          // 64 bits, all in: the bf16 long chunk 2.3e-3 (the output's rounding alone 1.7e-3), the fp16
+          // frame 2.9e-4 (2.1e-4).
           ph[y][e] = (T)p;
           if constexpr (EXACT && sizeof(T) == 2) pl[y][e] = (T)(p - (float)ph[y][e]);
         }
@@ -560,10 +563,13 @@ __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_keys
 // that all rows see, those that some see (the chunk's own tokens, later ones left out),
 // nothing else. Only the second kind is masked, and empty slots cost no tile.
 //
-// 4096 tokens x 4 heads, 8 groups, 128 dims, 12288 old and 4096 own slots, bf16: 975 us,
-// 987 TFLOP/s (a large library product: 1187); the sorting took it from 1275 to 1134.
-// 1560 x 8 rows, 3 groups, 64 dims, 4680 slots, fp16: 85 us, 529 TFLOP/s: per score the
-// exponential costs more than its MFMA share.
+// 4096 tokens x 4 heads, 8 groups, 128 dims, 12288 old and 4096 own slots, bf16: 975 us on the
+// fastest machine seen and 1056 on the slowest, 987 and 911 TFLOP/s (a large library product on
+// the former: 1187); the sorting took it from 1275 to 1134.
+// 1560 x 8 rows, 3 groups, 64 dims, 4680 slots, fp16: 85 to 88 us, 529 to 511 TFLOP/s. In two of five
+// cycles there neither an MFMA nor a vector instruction issues: every tile waits for its
+// maximum (over its scores, then the other half's, then the vote) before its first exponential,
+// and 588 workgroups lie uneven on 768 places.
 constexpr int kScan = 4096, kBlock = 64;
 template <typename T, int D>
 __global__ __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) void attend_rows_kernel(TokenCacheArgs c,
@@ -1032,8 +1038,8 @@ __global__ __launch_bounds__(256) void finish_kernel(TokenCacheArgs c, TokenAtte
 // workgroup's slots are taken in the order seen by every row, by some rows, empty, so
 // that a mask costs the waves with the call's own tokens alone. Where whole workgroups would
 // leave CUs idle, RW = 2 waves share their keys and take every other 32 rows (61 tokens x 4
-// heads, 6 groups, 1531 slots, fp32: 15 us against 19.5). The long chunk above: 678
-// us, 709 TFLOP/s; the frame 53 us.
+// heads, 6 groups, 1531 slots, fp32: 15 us against 19.5). The long chunk above: 678 to
+// 717 us, 709 to 670 TFLOP/s; the frame 53 us.
 template <typename T, int D, int RW>
 __global__ __launch_bounds__(256, D == 128 || RW == 2 ? 2 : 3) void weights_kernel(TokenCacheArgs c, TokenAttend a, TokenAttendPlan pl) {
   using TL = Tile<T, D>;
