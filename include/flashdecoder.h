@@ -556,9 +556,9 @@ fd_status fd_token_attend_workspace(const fd_token_cache* cache, int32_t heads, 
  *   workspace   16-byte aligned, at least fd_token_attend_workspace bytes; its contents
  *               mean nothing between calls. Calls that may overlap, and captured graphs
  *               that may be replayed at once, need one each.
- * scale > 0 and below FLT_MAX ln 2, decay finite. Scores, softmax statistics, output sums and weights
- * are fp32; for 16-bit caches the probabilities enter P V rounded to that type (for
- * few rows as a sum of two such values). Results do not change from run to run.
+ * scale > 0 and below FLT_MAX ln 2, decay finite. Scores, softmax statistics, output sums and
+ * weights are fp32; for 16-bit caches the probabilities enter P V rounded to that type, or, for
+ * n x heads / groups <= 64, as a sum of two such values. Results do not change from run to run.
  * heads / groups <= 256, n x heads / groups <= 2^24, batch x n x heads <= 2^28, batch x
  * groups x capacity <= 2^31, else UNSUPPORTED. */
 fd_status fd_token_attend_device(const fd_token_cache* cache, const void* q, const int64_t q_stride[3], int32_t heads,
